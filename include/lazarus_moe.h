@@ -336,6 +336,89 @@ int32_t lz_layer_backward(const lz_shape* shape, const lz_layer_buffers* buffers
  * where no buffers were given).  A string of the library; "" before any refusal. */
 const char* lz_layer_refused(void);
 
+/* ---------------------------------------------------------------- low-rank adapters beside a shared projection
+ *
+ * Fine-tuning and serving of many adapters on one frozen projection: every token names the adapter that its request uses, or
+ * none, and
+ *
+ *   y[t] = x[t] W + h[t] B_a,   h[t] = scale[a] x[t] A_a^T,   a = ids[t]        (no adapter: x[t] W)
+ *
+ * W dev [d_in, d_out] (input-major, as the experts' weights), a dev [n, rank, d_in], b dev [n, rank, d_out], scale dev [n] f32,
+ * x dev [T, d_in], y dev [T, d_out].  dtype: of x, y, h, w, a, b and their gradients; products are summed in fp32, h is rounded
+ * once to dtype, y once.  LZ_BF16 with d_in, d_out and rank multiples of 8 and 16-byte aligned tensors runs on bf16 matrix
+ * instructions; everything else on fp32 ones.
+ *   T >= 0, d_in, d_out >= 1, 1 <= rank <= 1024, 1 <= n <= 4096, T * max(d_in, d_out) < 2^40, LZ_ESHAPE otherwise. */
+typedef struct {
+  int32_t T, d_in, d_out, rank, n, dtype;
+} lz_adapter_shape;
+
+/* bits of the device status word written by lz_adapter_plan */
+enum { LZ_ADAPTER_BAD_ID = 1 /* an id that is neither -1 nor in [0, n): taken as none */ };
+
+/* Bytes of device workspace (256-byte aligned) of the calls below; 0 if the shape is invalid.  A workspace serves one call at a
+ * time.  lz_adapter_plan puts a batch's plan there, for the forward and backward calls that follow on it. */
+size_t lz_adapter_workspace_bytes(const lz_adapter_shape* shape);
+
+/* Which tokens use which adapter.  ids dev [T] i32, -1: none.  status_opt dev [1] i32 or NULL (out: 0 or LZ_ADAPTER_* bits). */
+int32_t lz_adapter_plan(const int32_t* ids, const lz_adapter_shape* shape, int32_t* status_opt, void* ws, size_t ws_bytes,
+                        void* stream);
+
+/* y as above for the batch that was planned last on ws.  h dev [T, rank] out: what the backward keeps of it (rows in an order of
+ * the library's own). */
+int32_t lz_adapter_forward(const void* x, const void* w, const void* a, const void* b, const float* scale,
+                           const lz_adapter_shape* shape, void* h, void* y, void* ws, size_t ws_bytes, void* stream);
+
+/* Gradients of lz_adapter_forward on the same plan (W is frozen):  dh[t] = scale[a] dy[t] B_a^T,
+ *   dx[t] = dy[t] W^T + dh[t] A_a,   da[a] = sum of dh[t]^T x[t],   db[a] = sum of h[t]^T dy[t]   over the tokens t of a,
+ * zero for an adapter without tokens.  The sums have a fixed order.
+ *   dy dev [T, d_out]; h dev [T, rank] from the forward; dx dev [T, d_in], da dev [n, rank, d_in], db dev [n, rank, d_out] out */
+int32_t lz_adapter_backward(const void* dy, const void* x, const void* h, const void* w, const void* a, const void* b,
+                            const float* scale, const lz_adapter_shape* shape, void* dx, void* da, void* db, void* ws,
+                            size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------- orthogonalised updates
+ *
+ * An update by the nearest orthogonal matrix rather than the gradient's own scale (as the Muon optimiser does), for stacks of
+ * matrices: experts' weights, adapters' factors.  From X = u / (|u| + eps), |u| the Frobenius norm, every step takes
+ *
+ *   X <- (c0 I + c1 G + c2 G^2) X,   G = X X^T  (over the shorter side)
+ *
+ * with its own three coefficients.  n matrices [rows, cols] of dtype, each on its own.
+ *   1 <= n <= 65535, rows, cols >= 1, rows * cols < 2^30, LZ_ESHAPE otherwise. */
+typedef struct {
+  int32_t n, rows, cols, dtype;
+} lz_orthogonal_shape;
+
+/* Bytes of device workspace (256-byte aligned) of the two calls below, one call at a time; 0 if the shape is invalid. */
+size_t lz_orthogonal_workspace_bytes(const lz_orthogonal_shape* shape);
+
+/* out[i] = the matrix g[i] after `steps` steps.  coef host [steps, 3], 1 <= steps <= 16; LZ_EINVAL for coefficients that can
+ * take a singular value of [0, 1], or an intermediate product, past 2.8.
+ *   g, out dev [n, rows, cols] of shape->dtype; they may be the same memory.  A matrix of zeros stays zero (eps > 0).
+ * Products take their factors in 16-bit floating point, of 11 bits where the result is rounded to bf16 and, for LZ_F32, in two
+ * parts of 11 bits each; sums are fp32. */
+int32_t lz_orthogonalize(const void* g, const lz_orthogonal_shape* shape, const float* coef, int32_t steps, float eps, void* out,
+                         void* ws, size_t ws_bytes, void* stream);
+
+typedef struct {
+  const float* coef; /* host [steps, 3] */
+  int32_t steps;
+  float eps;
+  double mu;           /* of the momentum */
+  double lr, weight_decay, scale;
+  int32_t nesterov;    /* 1: u = g + mu m, 0: u = m */
+} lz_orthogonal_options;
+
+/* One optimizer step of n matrices kept in fp32, and the copies of them that replicas train with:
+ *   m = mu momentum + g,  o = u after the steps above,  master_out = (1 - lr weight_decay) master - lr scale o,
+ *   slot_weights[s] = master_out[slot_expert[s]] rounded to shape->dtype, for slots s whose entry lies in [0, n)
+ * The products take their factors in two parts of 11 bits each, whatever shape->dtype.
+ *   g dev [n, rows, cols] of shape->dtype;  momentum, master, momentum_out, master_out dev [n, rows, cols] f32, where an
+ *   out may be its input's memory;  slot_expert dev [slots] i32, slot_weights dev [slots, rows, cols] of shape->dtype (slots = 0: none) */
+int32_t lz_orthogonal_step(const void* g, const float* momentum, const float* master, const int32_t* slot_expert, int32_t slots,
+                           const lz_orthogonal_shape* shape, const lz_orthogonal_options* options, float* momentum_out,
+                           float* master_out, void* slot_weights, void* ws, size_t ws_bytes, void* stream);
+
 /* ---------------------------------------------------------------- host planning */
 
 /* Replica allocation, Eq. 1 (Sec. 4.1): experts in ascending load t_e (ties: lower id)

@@ -6,4 +6,8 @@ step of the path runs in the library's kernels.  There is no CPU fallback: impor
 `binding` fails loudly if the shared library has not been built.
 """
 from .binding import *  # noqa: F401,F403
-from .binding import __all__  # noqa: F401
+from .finetune import *  # noqa: F401,F403
+from .binding import __all__ as _layer
+from .finetune import __all__ as _finetune
+
+__all__ = [*_layer, *_finetune]

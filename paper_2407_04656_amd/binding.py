@@ -151,6 +151,13 @@ def _load():
         "lz_layer_forward_train": (i32, [sp, vp, vp, vp, vp]),
         "lz_layer_backward": (i32, [sp, vp, vp, i32, vp]),
         "lz_layer_refused": (C.c_char_p, []),
+        "lz_adapter_workspace_bytes": (u64, [vp]),
+        "lz_adapter_plan": (i32, [vp, vp, vp, vp, u64, vp]),
+        "lz_adapter_forward": (i32, [vp, vp, vp, vp, vp, vp, vp, vp, vp, u64, vp]),
+        "lz_adapter_backward": (i32, [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, u64, vp]),
+        "lz_orthogonal_workspace_bytes": (u64, [vp]),
+        "lz_orthogonalize": (i32, [vp, vp, vp, i32, C.c_float, vp, vp, u64, vp]),
+        "lz_orthogonal_step": (i32, [vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, u64, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)

@@ -1,0 +1,231 @@
+// Products of the orthogonalised updates on the gfx950 matrix cores, fp16 in / fp32 accumulate.  Device code of
+// orthogonal.hip, not part of the C ABI.
+//
+// A step X <- q(G) X with q(s) = c0 + c1 s + c2 s^2, G = X X^T, is taken as
+//
+//   GRAM    H = X X^T - mu I                       mu = -c1 / (2 c2): q(s) = c2 (s - mu)^2 + q0, one square and no difference
+//   SQUARE  P = c2 H H + lin H + (q0 - rho) I      of nearly equal terms (lin = 0 then; mu = 0, lin = c1 where c2 does not allow it)
+//   APPLY   X' = rho X + P X
+//
+// Numbers are fp16 at 2^14 times their size (spectral norms are below 3.9: no element overflows, the 2^-25 that the smallest
+// fp16 step is off by counts nothing), in one plane (11 bits) or in two, the second holding what the first rounds off.  Products of
+// two planes are hi hi + hi lo + lo hi: three times the K loop, with other planes.  bf16 factors (8 bits) lose 1 to 3 % of the
+// result in five steps of the usual quintic; fp16 in one plane 0.1 %, and 0.13 to 0.3 % with the polynomial in its plain form (2-norm
+// of the error over that of the result, matrices of 16 x 4096 to 1408 x 2048), in two planes 2e-6, as fp32 does.
+#pragma once
+#include "gemm_narrow.h"
+
+namespace {
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+constexpr float kOrthoScale = 16384.f;
+
+enum { KIND_GRAM = 0, KIND_SQUARE = 1, KIND_APPLY = 2 };
+
+struct OrthoArgs {
+  const uint16_t* X;  // [planes][n][sp][lp]
+  uint16_t* H;        // [planes][n][sp][sp]
+  uint16_t* P;        // ...
+  uint16_t* out;      // APPLY: X'
+  float* residual;    // [n][sp]: what rounding took from H's diagonal (one plane)
+  int n, sp, lp;
+  float mu, c2, lin, diag, rho;  // diag = q0 - rho
+};
+
+__device__ __forceinline__ float f16_value(uint16_t b) { return (float)__builtin_bit_cast(_Float16, b); }
+__device__ __forceinline__ uint16_t f16_bits(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
+
+// Eight values of one row, to and from the planes.
+template <int PLANES>
+__device__ __forceinline__ void store_planes8(uint16_t* to, size_t plane, const float (&v)[8]) {
+  f16x8 hi, lo;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    hi[j] = (_Float16)v[j];
+    lo[j] = (_Float16)(v[j] - (float)hi[j]);
+  }
+  *(f16x8*)to = hi;
+  if constexpr (PLANES == 2) *(f16x8*)(to + plane) = lo;
+}
+template <int PLANES>
+__device__ __forceinline__ void load_planes8(const uint16_t* from, size_t plane, float (&v)[8]) {
+  const f16x8 hi = *(const f16x8*)from;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = (float)hi[j];
+  if constexpr (PLANES == 2) {
+    const f16x8 lo = *(const f16x8*)(from + plane);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] += (float)lo[j];
+  }
+}
+
+// 64 x 64 tiles, four waves of 32 x 32, a ring of four K steps of 64 as in gemm_narrow.h.  GRAM and SQUARE are symmetric: only tiles
+// on and below the diagonal are computed, and stored twice.  blockIdx.x = tile, blockIdx.y = matrix.
+template <int KIND, int PLANES>
+__global__ __launch_bounds__(256, 2) void ortho_narrow_kernel(OrthoArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr bool TB = KIND == KIND_APPLY;  // W k-major
+  constexpr int NS = kNarrowStages, kLoads = 4;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int sp = a.sp, lp = a.lp;
+  int tm, tn;
+  if constexpr (TB) {
+    const int cols = lp / kNarrow;
+    tm = blockIdx.x / cols;
+    tn = blockIdx.x % cols;
+  } else {  // the row tm of the triangle with tm (tm + 1) / 2 <= tile
+    tm = (int)((__fsqrt_rn(8.f * (float)blockIdx.x + 1.f) - 1.f) * 0.5f);
+    while ((tm + 1) * (tm + 2) / 2 <= (int)blockIdx.x) ++tm;
+    while (tm * (tm + 1) / 2 > (int)blockIdx.x) --tm;
+    tn = (int)blockIdx.x - tm * (tm + 1) / 2;
+  }
+  const int m0 = tm * kNarrow, n0 = tn * kNarrow;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave >> 1, wn = wave & 1;
+  const size_t large = (size_t)sp * lp, small = (size_t)sp * sp, at = blockIdx.y;
+  const uint16_t* const matA = KIND == KIND_GRAM ? a.X + at * large : KIND == KIND_SQUARE ? a.H + at * small : a.P + at * small;
+  const uint16_t* const matW = KIND == KIND_SQUARE ? a.H + at * small : a.X + at * large;
+  const size_t planeA = (KIND == KIND_GRAM ? large : small) * a.n, planeW = (KIND == KIND_SQUARE ? small : large) * a.n;
+  const int K = KIND == KIND_GRAM ? lp : sp, ldw = TB ? lp : K;
+  const uint32_t extentA = (uint32_t)((KIND == KIND_GRAM ? large : small) * 2), extentW = (uint32_t)((KIND == KIND_SQUARE ? small : large) * 2);
+  const int stepW = TB ? BK * ldw * 2 : BK * 2;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
+  int voffX[2], voffW[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int r = (wave * 2 + i) * 8 + (lane >> 3);
+    const int chunk = (lane & 7) ^ swz(r);
+    voffX[i] = (int)(((uint32_t)(m0 + r) * (uint32_t)K + (uint32_t)chunk * 8u) * 2u);
+    if constexpr (TB) voffW[i] = (int)(((uint32_t)r * (uint32_t)ldw + (uint32_t)(n0 + ((lane & 7) ^ swz_narrow(r)) * 8)) * 2u);
+    else voffW[i] = (int)(((uint32_t)(n0 + r) * (uint32_t)K + (uint32_t)chunk * 8u) * 2u);
+  }
+  const int k_steps = K / BK, all_steps = PLANES == 2 ? 3 * k_steps : k_steps;
+  int seg = 0, k = 0;  // of the next step to load: which pair of planes, step within it
+  auto issue = [&](bool real, int stage) {  // a step past the end writes zeros, without memory traffic
+    const i32x4 wa = rsrc_words(matA + (seg == 2 ? planeA : 0), real ? extentA : 0), ww = rsrc_words(matW + (seg == 1 ? planeW : 0), real ? extentW : 0);
+    const uint32_t lds = lds0 + stage * kNarrowStage;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) load16_to_lds(ww, lds + kNarrowOperand + (wave * 2 + i) * 1024, voffW[i], k * stepW);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) load16_to_lds(wa, lds + (wave * 2 + i) * 1024, voffX[i], k * BK * 2);
+    if (++k == k_steps) {
+      k = 0;
+      ++seg;
+    }
+  };
+  int fragoff[2], woff[2];
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks) {
+    const int r = lane & 15;
+    fragoff[ks] = r * kRowBytes + (((ks * 4 + (lane >> 4)) ^ swz(r)) << 4);
+  }
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    if constexpr (TB) {
+      const int q = lane & 15, kr = 8 * (lane >> 4) + (q >> 2);
+      woff[c] = kr * kRowBytes + ((q & 1) << 3) + (((((2 * wn + c) << 1) | ((q >> 1) & 1)) ^ swz_narrow(kr)) << 4);
+    } else {
+      woff[c] = (2 * wn + c) * 16 * kRowBytes;
+    }
+  }
+  auto read_x = [&](const char* st, int ks, int j) { return *(const f16x8*)(st + (2 * wm + j) * 16 * kRowBytes + fragoff[ks]); };
+  auto read_w = [&](const char* st, int ks, int c) {
+    if constexpr (TB) {
+      const char* p = st + kNarrowOperand + woff[c] + ks * 32 * kRowBytes;
+      const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)p);
+      const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(p + 4 * kRowBytes));
+      return __builtin_bit_cast(f16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+      return *(const f16x8*)(st + kNarrowOperand + woff[c] + fragoff[ks]);
+    }
+  };
+  f32x4 acc[2][2] = {};
+#pragma unroll
+  for (int s = 0; s < NS - 1; ++s) issue(s < all_steps, s);
+  int stage = 0;
+  for (int kt = 0; kt < all_steps; ++kt) {
+    constexpr int kAhead = (NS - 2) * kLoads;
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (kAhead & 15) | ((kAhead >> 4) << 14));  // this wave's loads of step kt are in LDS
+    __syncthreads();  // ... everyone's are; and nobody reads the stage of step kt - 1 any more
+    issue(kt + NS - 1 < all_steps, stage == 0 ? NS - 1 : stage - 1);
+    const char* const st = smem + stage * kNarrowStage;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      f16x8 x[2], w[2];
+#pragma unroll
+      for (int c = 0; c < 2; ++c) w[c] = read_w(st, ks, c);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) x[j] = read_x(st, ks, j);
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[c][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[c], x[j], acc[c][j], 0, 0, 0);
+    }
+    stage = stage + 1 == NS ? 0 : stage + 1;
+  }
+  // the trailing loads still write zeros into stages: drained by every wave before the tile overwrites them
+  __builtin_amdgcn_s_waitcnt(0x0F70);
+  __syncthreads();
+  // the tile, fp32, [row][column] through LDS, so that both it and its mirror image leave in 16-byte pieces
+  constexpr int kPitch = kNarrow + 1;
+  float* const tile = (float*)smem;
+#pragma unroll
+  for (int c = 0; c < 2; ++c)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int v = 0; v < 4; ++v)
+        tile[(32 * wm + 16 * j + (lane & 15)) * kPitch + 32 * wn + 16 * c + 4 * (lane >> 4) + v] = acc[c][j][v];
+  __syncthreads();
+  constexpr float kDown = 1.f / kOrthoScale;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int p = threadIdx.x + 256 * i, r = p >> 3, c = (p & 7) * 8;
+    float v[8];
+    if constexpr (KIND == KIND_APPLY) {
+      const size_t to = at * large + (size_t)(m0 + r) * lp + n0 + c;
+      float x[8];
+      load_planes8<PLANES>(a.X + to, planeW, x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = fmaf(a.rho, x[j], tile[r * kPitch + c + j] * kDown);
+      store_planes8<PLANES>(a.out + to, planeW, v);
+    } else {
+      // value of element (row, column) of the tile; `from`: of H, where it is read
+      auto finish = [&](float sum, int row, int col, float h) {
+        const bool on = m0 + row == n0 + col;
+        if constexpr (KIND == KIND_GRAM) return fmaf(sum, kDown, on ? -a.mu * kOrthoScale : 0.f);
+        if (PLANES == 1 && on) sum = fmaf(2.f * a.residual[at * sp + m0 + row], h, sum);
+        return fmaf(a.lin, h, fmaf(a.c2 * kDown, sum, on ? a.diag * kOrthoScale : 0.f));
+      };
+      const size_t to = at * small + (size_t)(m0 + r) * sp + n0 + c;
+      const bool with_h = KIND == KIND_SQUARE && (a.lin != 0.f || tm == tn);
+      uint16_t* const dst = KIND == KIND_GRAM ? a.H : a.P;
+      float h[8] = {};
+      if (with_h) load_planes8<PLANES>(a.H + to, planeA, h);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        v[j] = finish(tile[r * kPitch + c + j], r, c + j, h[j]);
+        if (KIND == KIND_GRAM && PLANES == 1 && m0 + r == n0 + c + j) a.residual[at * sp + m0 + r] = v[j] - f16_value(f16_bits(v[j]));
+      }
+      store_planes8<PLANES>(dst + to, KIND == KIND_GRAM ? small * a.n : planeA, v);
+      if (tm != tn) {
+        const size_t mirror = at * small + (size_t)(n0 + r) * sp + m0 + c;
+        if (with_h) load_planes8<PLANES>(a.H + mirror, planeA, h);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = finish(tile[(c + j) * kPitch + r], c + j, r, h[j]);
+        store_planes8<PLANES>(dst + mirror, KIND == KIND_GRAM ? small * a.n : planeA, v);
+      }
+    }
+  }
+#endif
+}
+
+template <int KIND, int PLANES>
+int32_t launch_ortho_narrow(const OrthoArgs& a, hipStream_t st) {
+  const int m = a.sp / kNarrow;
+  const long long tiles = KIND == KIND_APPLY ? (long long)m * (a.lp / kNarrow) : (long long)m * (m + 1) / 2;
+  hipLaunchKernelGGL((ortho_narrow_kernel<KIND, PLANES>), dim3((unsigned)tiles, (unsigned)a.n), dim3(256), kNarrowLds, st, a);
+  return lz::launch_status();
+}
+
+}  // namespace

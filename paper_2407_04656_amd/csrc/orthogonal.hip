@@ -1,0 +1,292 @@
+// Orthogonalised updates: Newton-Schulz steps of stacks of matrices, and the optimizer step around them.
+#include <cmath>
+
+#include "gemm_orthogonal.h"
+#include "gemm_f32.h"
+
+namespace {
+
+constexpr int kMostSteps = 16;
+constexpr double kMostNorm = 3.9;  // of what is kept in fp16: 3.9 * 2^14 < 65504
+constexpr int kNormBlocks = 64;    // partial sums of a matrix
+
+inline int up64(int v) { return (v + 63) / 64 * 64; }
+
+struct OrthoSize {
+  int n, rows, cols, sp, lp;
+  bool tall;  // rows > cols: X is the transpose
+};
+inline OrthoSize size_of(const lz_orthogonal_shape* s) {
+  const bool tall = s->rows > s->cols;
+  return OrthoSize{s->n, s->rows, s->cols, up64(tall ? s->cols : s->rows), up64(tall ? s->rows : s->cols), tall};
+}
+inline bool shape_ok(const lz_orthogonal_shape* s) {
+  if (!s || s->n < 1 || s->n > 65535 || s->rows < 1 || s->cols < 1 || (s->dtype != LZ_F32 && s->dtype != LZ_BF16)) return false;
+  if (s->rows >= (1 << 30) || s->cols >= (1 << 30)) return false;
+  const OrthoSize z = size_of(s);
+  return (long long)z.sp * z.lp < (1ll << 30);
+}
+
+struct OrthoWorkspace {
+  double* sums;     // [n, kNormBlocks]
+  float* residual;  // [n, sp]
+  uint16_t *X[2], *H, *P;  // two planes each
+  size_t bytes;
+};
+OrthoWorkspace carve(void* ws, const lz_orthogonal_shape* s) {
+  const OrthoSize z = size_of(s);
+  OrthoWorkspace w{};
+  char* p = (char*)ws;
+  auto take = [&](size_t bytes) {
+    char* r = p;
+    p += lz::align256(bytes);
+    return r;
+  };
+  w.sums = (double*)take(sizeof(double) * z.n * kNormBlocks);
+  w.residual = (float*)take(sizeof(float) * z.n * z.sp);
+  for (auto& x : w.X) x = (uint16_t*)take(4 * (size_t)z.n * z.sp * z.lp);
+  w.H = (uint16_t*)take(4 * (size_t)z.n * z.sp * z.sp);
+  w.P = (uint16_t*)take(4 * (size_t)z.n * z.sp * z.sp);
+  w.bytes = size_t(p - (char*)ws);
+  return w;
+}
+
+// What is orthogonalised: the gradient, or the gradient and its momentum.
+struct Source {
+  const void* g;
+  const float* momentum;  // the new one, where there is one
+  float mu;
+  int nesterov;
+};
+template <typename Elem, bool UPDATE>
+__device__ __forceinline__ float source_value(const Source& s, size_t i) {
+  if constexpr (!UPDATE) return load_elem<Elem>((const Elem*)s.g + i);
+  else return s.nesterov ? fmaf(s.mu, s.momentum[i], load_elem<Elem>((const Elem*)s.g + i)) : s.momentum[i];
+}
+
+// Sums of squares in 64 bits (fp32 inputs of any size), kNormBlocks of every matrix; UPDATE: the new momentum on the way.
+template <typename Elem, bool UPDATE>
+__global__ __launch_bounds__(256) void norm_kernel(Source s, const float* old, float* momentum, size_t elems,
+                                                   double* __restrict__ sums) {
+  __shared__ double waves[4];
+  const size_t base = blockIdx.y * elems;
+  double sum = 0.0;
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < elems; i += kNormBlocks * 256) {
+    float u;
+    if constexpr (UPDATE) {
+      const float g = load_elem<Elem>((const Elem*)s.g + base + i), m = fmaf(s.mu, old[base + i], g);
+      momentum[base + i] = m;
+      u = s.nesterov ? fmaf(s.mu, m, g) : m;
+    } else {
+      u = load_elem<Elem>((const Elem*)s.g + base + i);
+    }
+    sum = fma((double)u, (double)u, sum);
+  }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
+  if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) sums[(size_t)blockIdx.y * kNormBlocks + blockIdx.x] = waves[0] + waves[1] + waves[2] + waves[3];
+}
+
+// 64 x 64 of a matrix as it lies -> X, transposed where it is tall, scaled to norm 1 (times 2^14), zeros around it.
+template <typename Elem, bool UPDATE, int PLANES>
+__global__ __launch_bounds__(256) void load_kernel(Source s, OrthoSize z, const double* __restrict__ sums, float eps, uint16_t* __restrict__ X) {
+  __shared__ float tile[64][65];
+  const int lane = threadIdx.x & 63;
+  double total = sums[(size_t)blockIdx.y * kNormBlocks + lane];
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) total += __shfl_xor(total, off, 64);
+  const double norm = sqrt(total) + (double)eps;
+  const float inv = (float)(1.0 / norm);
+  const int tiles_c = (z.tall ? z.sp : z.lp) / 64, r0 = blockIdx.x / tiles_c * 64, c0 = blockIdx.x % tiles_c * 64;
+  const size_t base = (size_t)blockIdx.y * z.rows * z.cols;
+  for (int i = 0; i < 16; ++i) {
+    const int r = i * 4 + (threadIdx.x >> 6), row = r0 + r, col = c0 + lane;
+    float v = 0.f;
+    if (row < z.rows && col < z.cols) v = source_value<Elem, UPDATE>(s, base + (size_t)row * z.cols + col) * inv;
+    tile[r][lane] = v * kOrthoScale;
+  }
+  __syncthreads();
+  const size_t plane = (size_t)z.n * z.sp * z.lp;
+  uint16_t* const to = X + (size_t)blockIdx.y * z.sp * z.lp;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int p = threadIdx.x + 256 * i, r = p >> 3, c = (p & 7) * 8;
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = z.tall ? tile[c + j][r] : tile[r][c + j];
+    const int row = (z.tall ? c0 : r0) + r, col = (z.tall ? r0 : c0) + c;
+    store_planes8<PLANES>(to + (size_t)row * z.lp + col, plane, v);
+  }
+}
+
+struct Update {
+  float keep, rate;  // 1 - lr weight_decay, lr scale
+  const float* master;
+  float* master_out;
+  const int32_t* slot_expert;
+  int slots;
+  void* slot_weights;
+};
+
+// X -> the result as it lies; UPDATE: the weights, and their copies in the slots.
+template <typename Elem, bool UPDATE, int PLANES>
+__global__ __launch_bounds__(256) void finish_kernel(const uint16_t* __restrict__ X, OrthoSize z, Elem* __restrict__ out, Update u) {
+  __shared__ float tile[64][65];
+  const int tiles_c = (z.tall ? z.sp : z.lp) / 64, r0 = blockIdx.x / tiles_c * 64, c0 = blockIdx.x % tiles_c * 64;
+  const size_t plane = (size_t)z.n * z.sp * z.lp;
+  const uint16_t* const from = X + (size_t)blockIdx.y * z.sp * z.lp;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int p = threadIdx.x + 256 * i, r = p >> 3, c = (p & 7) * 8;
+    const int row = (z.tall ? c0 : r0) + r, col = (z.tall ? r0 : c0) + c;
+    float v[8];
+    load_planes8<PLANES>(from + (size_t)row * z.lp + col, plane, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (z.tall) tile[c + j][r] = v[j];
+      else tile[r][c + j] = v[j];
+    }
+  }
+  __syncthreads();
+  const int lane = threadIdx.x & 63;
+  const size_t elems = (size_t)z.rows * z.cols, base = blockIdx.y * elems;
+  if constexpr (UPDATE) {
+    for (int i = 0; i < 16; ++i) {
+      const int r = i * 4 + (threadIdx.x >> 6), row = r0 + r, col = c0 + lane;
+      if (row < z.rows && col < z.cols) {
+        const size_t at = base + (size_t)row * z.cols + col;
+        const float v = fmaf(u.keep, u.master[at], -u.rate * (tile[r][lane] * (1.f / kOrthoScale)));
+        u.master_out[at] = v;
+        tile[r][lane] = v;
+      }
+    }
+    // (a thread reads back what it wrote itself)
+    for (int s0 = 0; s0 < u.slots; s0 += 64) {
+      const int s = s0 + lane;
+      unsigned long long mine = __ballot(s < u.slots && u.slot_expert[s < u.slots ? s : 0] == (int)blockIdx.y);
+      for (; mine != 0; mine &= mine - 1) {
+        Elem* const to = (Elem*)u.slot_weights + (size_t)(s0 + __ffsll((long long)mine) - 1) * elems;
+        for (int i = 0; i < 16; ++i) {
+          const int r = i * 4 + (threadIdx.x >> 6), row = r0 + r, col = c0 + lane;
+          if (row < z.rows && col < z.cols) store_elem<Elem>(to + (size_t)row * z.cols + col, tile[r][lane]);
+        }
+      }
+    }
+  } else {
+    for (int i = 0; i < 16; ++i) {
+      const int r = i * 4 + (threadIdx.x >> 6), row = r0 + r, col = c0 + lane;
+      if (row < z.rows && col < z.cols) store_elem<Elem>(out + base + (size_t)row * z.cols + col, tile[r][lane] * (1.f / kOrthoScale));
+    }
+  }
+}
+
+// The steps' constants.
+struct Step {
+  float mu, c2, lin, diag, rho;
+};
+
+// false: coefficients that can lead past kMostNorm.  Singular values start in [0, 1]; a step takes x to x q(x^2).
+bool plan_steps(const float* coef, int steps, int planes, Step* out) {
+  double most = 1.0;
+  for (int k = 0; k < steps; ++k) {
+    const double a = coef[3 * k], b = coef[3 * k + 1], c = coef[3 * k + 2];
+    if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
+    const double top = most * most;
+    double mu = c != 0.0 ? -b / (2 * c) : 0.0;
+    if (!(std::fabs(mu) <= 2.0)) mu = 0.0;  // far off [0, 1]: H would be mu and little else
+    // rho X + P X: P is small, and its rounding with it, where q is near rho, which the last steps take near 1; not above c0, which q
+    // is for small singular values.  One plane: the first steps enlarge those, and an 11-bit diagonal of P would be what is off most.
+    const double rho = planes == 1 && 2 * k < steps - 1 ? a : std::fmin(a, 1.0);
+    const double q0 = a + b * mu + c * mu * mu;
+    auto q = [&](double s) { return a + b * s + c * s * s; };
+    double p = std::fmax(std::fabs(q(0) - rho), std::fabs(q(top) - rho));
+    if (c != 0.0 && -b / (2 * c) > 0 && -b / (2 * c) < top) p = std::fmax(p, std::fabs(q(-b / (2 * c)) - rho));
+    double next = most * std::fabs(q(top));
+    auto at = [&](double y) {  // y = x^2 with (x q(x^2))' = a + 3 b y + 5 c y^2 = 0
+      if (y > 0 && y < top) next = std::fmax(next, std::sqrt(y) * std::fabs(q(y)));
+    };
+    if (c != 0.0) {
+      const double d = 9 * b * b - 20 * a * c;
+      if (d >= 0) {
+        at((-3 * b + std::sqrt(d)) / (10 * c));
+        at((-3 * b - std::sqrt(d)) / (10 * c));
+      }
+    } else if (b != 0.0) {
+      at(-a / (3 * b));
+    }
+    const double h = std::fmax(std::fabs(mu), std::fabs(top - mu));
+    if (!(h <= kMostNorm && p <= kMostNorm && next <= kMostNorm)) return false;
+    out[k] = Step{(float)mu, (float)c, mu != 0.0 ? 0.f : (float)b, (float)(q0 - rho), (float)rho};
+    most = next;
+  }
+  return true;
+}
+
+template <typename Elem, bool UPDATE, int PLANES>
+int32_t run(const Source& source, const float* old, const lz_orthogonal_shape* shape, const Step* steps, int n_steps, float eps, void* out,
+            const Update& update, const OrthoWorkspace& w, hipStream_t st) {
+  const OrthoSize z = size_of(shape);
+  const unsigned tiles = (unsigned)((size_t)z.sp * z.lp / 4096);
+  const size_t elems = (size_t)z.rows * z.cols;
+  hipLaunchKernelGGL((norm_kernel<Elem, UPDATE>), dim3(kNormBlocks, z.n), dim3(256), 0, st, source, old, (float*)source.momentum, elems, w.sums);
+  hipLaunchKernelGGL((load_kernel<Elem, UPDATE, PLANES>), dim3(tiles, z.n), dim3(256), 0, st, source, z, w.sums, eps, w.X[0]);
+  int32_t rc = lz::launch_status();
+  int cur = 0;
+  for (int k = 0; k < n_steps && rc == LZ_OK; ++k, cur ^= 1) {
+    const Step& s = steps[k];
+    const OrthoArgs a{w.X[cur], w.H, w.P, w.X[cur ^ 1], w.residual, z.n, z.sp, z.lp, s.mu, s.c2, s.lin, s.diag, s.rho};
+    rc = launch_ortho_narrow<KIND_GRAM, PLANES>(a, st);
+    if (rc == LZ_OK) rc = launch_ortho_narrow<KIND_SQUARE, PLANES>(a, st);
+    if (rc == LZ_OK) rc = launch_ortho_narrow<KIND_APPLY, PLANES>(a, st);
+  }
+  if (rc != LZ_OK) return rc;
+  hipLaunchKernelGGL((finish_kernel<Elem, UPDATE, PLANES>), dim3(tiles, z.n), dim3(256), 0, st, w.X[cur], z, (Elem*)out, update);
+  return lz::launch_status();
+}
+
+int32_t check(const lz_orthogonal_shape* s, const float* coef, int32_t steps, float eps, int planes, void* ws, size_t ws_bytes, OrthoWorkspace* w,
+              Step* plan) {
+  if (!shape_ok(s)) return LZ_ESHAPE;
+  if (!coef || steps < 1 || steps > kMostSteps || !(eps >= 0.f) || !std::isfinite(eps) || !plan_steps(coef, steps, planes, plan)) return LZ_EINVAL;
+  *w = carve(ws, s);
+  if (!ws || (uintptr_t)ws % 256 != 0 || ws_bytes < w->bytes) return LZ_EWORKSPACE;
+  return LZ_OK;
+}
+
+}  // namespace
+
+extern "C" size_t lz_orthogonal_workspace_bytes(const lz_orthogonal_shape* shape) {
+  return shape_ok(shape) ? carve(nullptr, shape).bytes : 0;
+}
+
+extern "C" int32_t lz_orthogonalize(const void* g, const lz_orthogonal_shape* shape, const float* coef, int32_t steps, float eps, void* out,
+                                    void* ws, size_t ws_bytes, void* stream) {
+  OrthoWorkspace w;
+  Step plan[kMostSteps];
+  const int32_t rc = check(shape, coef, steps, eps, shape && shape->dtype == LZ_F32 ? 2 : 1, ws, ws_bytes, &w, plan);
+  if (rc != LZ_OK) return rc;
+  if (!g || !out) return LZ_EINVAL;
+  const Source source{g, nullptr, 0.f, 0};
+  hipStream_t st = (hipStream_t)stream;
+  return shape->dtype == LZ_F32 ? run<float, false, 2>(source, nullptr, shape, plan, steps, eps, out, Update{}, w, st)
+                                : run<uint16_t, false, 1>(source, nullptr, shape, plan, steps, eps, out, Update{}, w, st);
+}
+
+extern "C" int32_t lz_orthogonal_step(const void* g, const float* momentum, const float* master, const int32_t* slot_expert, int32_t slots,
+                                      const lz_orthogonal_shape* shape, const lz_orthogonal_options* options, float* momentum_out,
+                                      float* master_out, void* slot_weights, void* ws, size_t ws_bytes, void* stream) {
+  if (!options) return LZ_EINVAL;
+  OrthoWorkspace w;
+  Step plan[kMostSteps];
+  const int32_t rc = check(shape, options->coef, options->steps, options->eps, 2, ws, ws_bytes, &w, plan);
+  if (rc != LZ_OK) return rc;
+  if (!g || !momentum || !master || !momentum_out || !master_out || slots < 0 || (slots > 0 && (!slot_expert || !slot_weights))) return LZ_EINVAL;
+  const Source source{g, momentum_out, (float)options->mu, options->nesterov};
+  const Update update{(float)(1.0 - options->lr * options->weight_decay), (float)(options->lr * options->scale), master, master_out, slot_expert,
+                      slots, slot_weights};
+  hipStream_t st = (hipStream_t)stream;
+  return shape->dtype == LZ_F32 ? run<float, true, 2>(source, momentum, shape, plan, options->steps, options->eps, nullptr, update, w, st)
+                                : run<uint16_t, true, 2>(source, momentum, shape, plan, options->steps, options->eps, nullptr, update, w, st);
+}

@@ -1,0 +1,264 @@
+"""Fine-tuning and serving of many low-rank adapters beside a shared projection, and orthogonalised updates of stacks of
+matrices: the calls of the C ABI with the same names, and an object each that owns the buffers.
+
+    projection = AdapterProjection(AdapterShape(T, d_in, d_out, rank, n, LZ_BF16))
+    projection.set_weights(w, a, b, scale)
+    projection.plan(ids)                       # the adapter of every token, -1: none
+    y = projection.forward(x)
+    dx, da, db = projection.backward(dy)       # after enable_training()
+
+    update = OrthogonalUpdate(OrthogonalShape(n, rows, cols, LZ_BF16))
+    out = update.orthogonalize(g)
+    momentum, master, slots = update.step(g, momentum, master, slot_expert, lr=2e-3, weight_decay=0.1)
+"""
+from __future__ import annotations
+
+import ctypes as C
+from dataclasses import dataclass
+
+import numpy as np
+
+from .binding import LZ_EINVAL, LZ_ESHAPE, LZ_F32, LzError, _check, _ptr, _stream, lib
+
+__all__ = [
+    "AdapterShape", "AdapterProjection", "OrthogonalShape", "OrthogonalUpdate", "LZ_ADAPTER_BAD_ID", "NEWTON_SCHULZ_5",
+    "lz_adapter_workspace_bytes", "lz_adapter_plan", "lz_adapter_forward", "lz_adapter_backward",
+    "lz_orthogonal_workspace_bytes", "lz_orthogonalize", "lz_orthogonal_step",
+]
+
+LZ_ADAPTER_BAD_ID = 1
+# the quintic that takes singular values of (0, 1] near 1 in five steps (K. Jordan et al., Muon, 2024)
+NEWTON_SCHULZ_5 = ((3.4445, -4.7750, 2.0315),) * 5
+
+
+class _AdapterShape(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("T", "d_in", "d_out", "rank", "n", "dtype")]
+
+
+class _OrthogonalShape(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n", "rows", "cols", "dtype")]
+
+
+class _OrthogonalOptions(C.Structure):
+    _fields_ = [("coef", C.c_void_p), ("steps", C.c_int32), ("eps", C.c_float), ("mu", C.c_double), ("lr", C.c_double),
+                ("weight_decay", C.c_double), ("scale", C.c_double), ("nesterov", C.c_int32)]
+
+
+class _ByReference:
+    """A shape's C struct by reference, built once: a shape does not change."""
+
+    def _arg(self):
+        ref = self.__dict__.get("_ref")
+        if ref is None:
+            ref = C.byref(self.c_struct())
+            object.__setattr__(self, "_ref", ref)
+        return ref
+
+    def __getstate__(self):
+        return {n: v for n, v in self.__dict__.items() if n != "_ref"}  # an address is of this process
+
+
+@dataclass(frozen=True)
+class AdapterShape(_ByReference):
+    T: int
+    d_in: int
+    d_out: int
+    rank: int
+    n: int
+    dtype: int
+
+    def c_struct(self):
+        return _AdapterShape(self.T, self.d_in, self.d_out, self.rank, self.n, self.dtype)
+
+
+@dataclass(frozen=True)
+class OrthogonalShape(_ByReference):
+    n: int
+    rows: int
+    cols: int
+    dtype: int
+
+    def c_struct(self):
+        return _OrthogonalShape(self.n, self.rows, self.cols, self.dtype)
+
+
+def _torch_dtype(dtype):
+    import torch
+    return torch.float32 if dtype == LZ_F32 else torch.bfloat16
+
+
+def _expect(where, *tensors):
+    """(tensor, shape, dtype, device): what does not fit is refused before an address is taken."""
+    for t, shape, dtype, device in tensors:
+        if t is None or t.dtype != dtype or t.device != device:
+            raise LzError(LZ_EINVAL, where)
+        if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+            raise LzError(LZ_ESHAPE, where)
+
+
+def _current(stream):
+    return _stream() if stream is None else stream
+
+
+# ------------------------------------------------------------------ the calls
+def lz_adapter_workspace_bytes(shape) -> int:
+    return int(lib.lz_adapter_workspace_bytes(shape._arg()))
+
+
+def lz_adapter_plan(ids, shape, status_opt, ws, ws_bytes, stream=None):
+    _check(lib.lz_adapter_plan(_ptr(ids), shape._arg(), _ptr(status_opt), _ptr(ws), ws_bytes, _current(stream)), "lz_adapter_plan")
+
+
+def lz_adapter_forward(x, w, a, b, scale, shape, h, y, ws, ws_bytes, stream=None):
+    _check(lib.lz_adapter_forward(_ptr(x), _ptr(w), _ptr(a), _ptr(b), _ptr(scale), shape._arg(), _ptr(h), _ptr(y), _ptr(ws), ws_bytes,
+                                  _current(stream)), "lz_adapter_forward")
+
+
+def lz_adapter_backward(dy, x, h, w, a, b, scale, shape, dx, da, db, ws, ws_bytes, stream=None):
+    _check(lib.lz_adapter_backward(_ptr(dy), _ptr(x), _ptr(h), _ptr(w), _ptr(a), _ptr(b), _ptr(scale), shape._arg(), _ptr(dx),
+                                   _ptr(da), _ptr(db), _ptr(ws), ws_bytes, _current(stream)), "lz_adapter_backward")
+
+
+def _coefficients(coef):
+    c = np.ascontiguousarray(np.asarray(coef, dtype=np.float32))
+    if c.ndim != 2 or c.shape[1] != 3:
+        raise LzError(LZ_EINVAL, "coefficients [steps, 3]")
+    return c
+
+
+def lz_orthogonal_workspace_bytes(shape) -> int:
+    return int(lib.lz_orthogonal_workspace_bytes(shape._arg()))
+
+
+def lz_orthogonalize(g, shape, coef, eps, out, ws, ws_bytes, stream=None):
+    c = _coefficients(coef)
+    _check(lib.lz_orthogonalize(_ptr(g), shape._arg(), c.ctypes.data, len(c), eps, _ptr(out), _ptr(ws), ws_bytes, _current(stream)),
+           "lz_orthogonalize")
+
+
+def lz_orthogonal_step(g, momentum, master, slot_expert, shape, momentum_out, master_out, slot_weights, ws, ws_bytes, *, coef, eps, mu,
+                       lr, weight_decay, scale, nesterov, stream=None):
+    c = _coefficients(coef)
+    options = _OrthogonalOptions(c.ctypes.data, len(c), eps, mu, lr, weight_decay, scale, nesterov)
+    slots = 0 if slot_expert is None else slot_expert.numel()
+    _check(lib.lz_orthogonal_step(_ptr(g), _ptr(momentum), _ptr(master), _ptr(slot_expert), slots, shape._arg(), C.addressof(options),
+                                  _ptr(momentum_out), _ptr(master_out), _ptr(slot_weights), _ptr(ws), ws_bytes, _current(stream)),
+           "lz_orthogonal_step")
+
+
+# ------------------------------------------------------------------ the objects
+class AdapterProjection:
+    """A frozen projection with the adapters of many requests beside it; owns the buffers of one shape."""
+
+    def __init__(self, shape: AdapterShape, device="cuda:0"):
+        import torch
+        self.shape, self.device = shape, torch.device(device)
+        self.ws_bytes = lz_adapter_workspace_bytes(shape)
+        if self.ws_bytes == 0:
+            raise LzError(LZ_ESHAPE, "lz_adapter_workspace_bytes")
+        dt = self._dtype = _torch_dtype(shape.dtype)
+        self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.device)
+        self.h = torch.empty((shape.T, shape.rank), dtype=dt, device=self.device)
+        self.y = torch.empty((shape.T, shape.d_out), dtype=dt, device=self.device)
+        self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self.w = self.a = self.b = self.scale = self.ids = self.x = None
+        self.dx = self.da = self.db = None
+
+    def set_weights(self, w, a, b, scale):
+        """w [d_in, d_out]; a [n, rank, d_in], b [n, rank, d_out]: the adapters' factors; scale [n] fp32.  Kept by reference:
+        factors that an optimizer changes in place are those of the next pass."""
+        import torch
+        s, dt, dev = self.shape, self._dtype, self.device
+        _expect("AdapterProjection.set_weights", (w, (s.d_in, s.d_out), dt, dev), (a, (s.n, s.rank, s.d_in), dt, dev),
+                (b, (s.n, s.rank, s.d_out), dt, dev), (scale, (s.n,), torch.float32, dev))
+        self.w, self.a, self.b, self.scale = w, a, b, scale
+
+    def plan(self, ids):
+        """The adapter of every token of the batch, int32 [T], -1 for none.  Other ids count as none and set a bit of `status`."""
+        import torch
+        _expect("AdapterProjection.plan", (ids, (self.shape.T,), torch.int32, self.device))
+        lz_adapter_plan(ids, self.shape, self.status, self.ws, self.ws_bytes)
+        self.ids = ids
+
+    def forward(self, x):
+        """y of the planned batch; x is kept by reference for backward()."""
+        s = self.shape
+        if self.ids is None or self.w is None:
+            raise LzError(LZ_EINVAL, "AdapterProjection.forward before set_weights and plan")
+        _expect("AdapterProjection.forward", (x, (s.T, s.d_in), self._dtype, self.device))
+        lz_adapter_forward(x, self.w, self.a, self.b, self.scale, s, self.h, self.y, self.ws, self.ws_bytes)
+        self.x = x
+        return self.y
+
+    def enable_training(self):
+        """Allocate the gradients."""
+        import torch
+        s, dt, dev = self.shape, self._dtype, self.device
+        self.dx = torch.empty((s.T, s.d_in), dtype=dt, device=dev)
+        self.da = torch.empty((s.n, s.rank, s.d_in), dtype=dt, device=dev)
+        self.db = torch.empty((s.n, s.rank, s.d_out), dtype=dt, device=dev)
+
+    def backward(self, dy):
+        """(dx, da, db) of the last forward(); adapters without a token get zeros."""
+        s = self.shape
+        if self.x is None or self.dx is None:
+            raise LzError(LZ_EINVAL, "AdapterProjection.backward before enable_training and forward")
+        _expect("AdapterProjection.backward", (dy, (s.T, s.d_out), self._dtype, self.device))
+        lz_adapter_backward(dy, self.x, self.h, self.w, self.a, self.b, self.scale, s, self.dx, self.da, self.db, self.ws, self.ws_bytes)
+        return self.dx, self.da, self.db
+
+
+class OrthogonalUpdate:
+    """Orthogonalised updates of n matrices [rows, cols]; owns the workspace and, where the caller gives none, the results."""
+
+    def __init__(self, shape: OrthogonalShape, device="cuda:0", coef=NEWTON_SCHULZ_5, eps=1e-7):
+        import torch
+        self.shape, self.device, self.coef, self.eps = shape, torch.device(device), _coefficients(coef), float(eps)
+        self.ws_bytes = lz_orthogonal_workspace_bytes(shape)
+        if self.ws_bytes == 0:
+            raise LzError(LZ_ESHAPE, "lz_orthogonal_workspace_bytes")
+        self._dtype = _torch_dtype(shape.dtype)
+        self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.device)
+        self._size = (shape.n, shape.rows, shape.cols)
+        self.out = self.momentum = self.master = self.slot_weights = None
+
+    def orthogonalize(self, g, out=None):
+        """The matrices of g after the steps; `out` may be g."""
+        import torch
+        if out is None:
+            if self.out is None:
+                self.out = torch.empty(self._size, dtype=self._dtype, device=self.device)
+            out = self.out
+        _expect("OrthogonalUpdate.orthogonalize", (g, self._size, self._dtype, self.device), (out, self._size, self._dtype, self.device))
+        lz_orthogonalize(g, self.shape, self.coef, self.eps, out, self.ws, self.ws_bytes)
+        return out
+
+    def step(self, g, momentum, master, slot_expert=None, *, mu=0.95, lr=2e-2, weight_decay=0.0, scale=1.0, nesterov=True,
+             momentum_out=None, master_out=None, slot_weights=None):
+        """One optimizer step: the new momentum and weights (fp32; into buffers of this object, or into *_out, which may be the
+        inputs themselves), and the slots' copies of the weights (None without slot_expert)."""
+        import torch
+        n, f32, dev = self.shape.n, torch.float32, self.device
+
+        def buffer(name, given, size, dtype):
+            if given is not None:
+                return given
+            own = getattr(self, name)
+            if own is None or tuple(own.shape) != size:
+                own = torch.empty(size, dtype=dtype, device=dev)
+                setattr(self, name, own)
+            return own
+
+        momentum_out = buffer("momentum", momentum_out, self._size, f32)
+        master_out = buffer("master", master_out, self._size, f32)
+        where = "OrthogonalUpdate.step"
+        if slot_expert is not None:
+            slots_size = (slot_expert.numel(),) + self._size[1:]
+            slot_weights = buffer("slot_weights", slot_weights, slots_size, self._dtype)
+            _expect(where, (slot_expert, (slot_expert.numel(),), torch.int32, dev), (slot_weights, slots_size, self._dtype, dev))
+        elif slot_weights is not None:
+            raise LzError(LZ_EINVAL, where)
+        _expect(where, (g, self._size, self._dtype, dev), *((t, self._size, f32, dev) for t in (momentum, master, momentum_out, master_out)))
+        lz_orthogonal_step(g, momentum, master, slot_expert, self.shape, momentum_out, master_out, slot_weights, self.ws, self.ws_bytes,
+                           coef=self.coef, eps=self.eps, mu=mu, lr=lr, weight_decay=weight_decay, scale=scale, nesterov=nesterov)
+        return momentum_out, master_out, slot_weights
