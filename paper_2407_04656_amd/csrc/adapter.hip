@@ -1,5 +1,6 @@
 // Low-rank adapters of many requests beside a shared projection: y = x W + scale_a (x A_a^T) B_a for the adapter a of
 // every token, and its gradients.
+#include "gemm_adapter.h"
 #include "gemm_split.h"
 
 namespace {
@@ -22,6 +23,27 @@ inline int chunk_tokens(int T) {  // at most 256 chunks of whole waves
 }
 inline int chunks_of(int T) { return (T + chunk_tokens(T) - 1) / chunk_tokens(T); }
 
+// Shapes on the bf16 kernels: rows of whole 16-byte pieces, every tensor within 31-bit byte offsets.
+inline bool whole_pieces(const lz_adapter_shape* s) {
+  const long long d = s->d_in > s->d_out ? s->d_in : s->d_out, most = (1ll << 30) - 4096;  // elements
+  return s->dtype == LZ_BF16 && s->d_in % 8 == 0 && s->d_out % 8 == 0 && s->rank % 8 == 0 && s->T * d < most &&
+         (long long)s->d_in * s->d_out < most && (long long)s->n * s->rank * d < most && (long long)s->T * s->rank < most;
+}
+// (the wide kernel's first two K steps are the base's)
+inline bool narrow_tiles(const lz_adapter_shape* s, int n_out, int K) { return use_narrow(s->T, 1, n_out) || K <= BK; }
+// Workgroups that share a narrow tile's sum: so many that the chip's 512 places are taken, four K steps at least each.
+inline int splits_of(const lz_adapter_shape* s, int n_out, int K) {
+  const long long tiles = (long long)ceil_div(s->T, kNarrow) * ceil_div(n_out, kNarrow), most = ceil_div(ceil_div(K, BK), 4);
+  const long long fill = 512 / (tiles > 0 ? tiles : 1);
+  return (int)(fill < 1 ? 1 : fill < most ? fill : most);
+}
+// Rows of a unit of the factors' gradients.
+inline int factor_chunk(int T) {
+  const int even = (T / 16 + 63) / 64 * 64;
+  return even < 256 ? 256 : even < kMostChunk ? even : kMostChunk;
+}
+inline int factor_units(const lz_adapter_shape* s) { return s->T / factor_chunk(s->T) + s->n; }
+
 struct AdapterWorkspace {
   int32_t* ids;      // [T], -1: none
   int32_t* counts;   // [chunks, n + 1], then where a chunk's tokens of an adapter go, from the adapter's first row on
@@ -35,6 +57,12 @@ struct AdapterWorkspace {
   float* low;        // [T, rank] before the scale
   void* dh;          // [T, rank]
   float* sum;        // [T, max(d_in, d_out)]
+  // shapes on the bf16 kernels
+  AdapterLists lists;
+  int32_t *unit_first, *unit_adapter;
+  float* part;          // of split sums
+  float* factor_part[2];
+  uint16_t* at;         // [n, d_in, rank]
   size_t bytes;
 };
 
@@ -62,6 +90,27 @@ AdapterWorkspace carve(void* ws, const lz_adapter_shape* s) {
   w.low = (float*)take(4 * T * s->rank);
   w.dh = take(eb * T * s->rank);
   w.sum = (float*)take(4 * T * d);
+  if (whole_pieces(s)) {
+    const size_t blocks = (T + 255) / 256, units = factor_units(s);
+    w.lists.count256 = (int32_t*)take(4 * blocks);
+    w.lists.list256 = (int32_t*)take(4 * 256 * blocks);
+    w.lists.local256 = (uint8_t*)take(256 * blocks);
+    w.lists.count64 = (int32_t*)take(4 * 4 * blocks);
+    w.lists.list64 = (int32_t*)take(4 * 256 * blocks);
+    w.lists.local64 = (uint8_t*)take(256 * blocks);
+    w.unit_first = (int32_t*)take(4 * ((size_t)s->n + 1));
+    w.unit_adapter = (int32_t*)take(4 * units);
+    size_t part = 0;
+    for (int way = 0; way < 2; ++way) {
+      const int n_out = way ? s->d_in : s->d_out, K = way ? s->d_out : s->d_in, splits = splits_of(s, n_out, K);
+      const size_t bytes = narrow_tiles(s, n_out, K) && splits > 1 ? 4 * (size_t)splits * T * n_out : 0;
+      if (bytes > part) part = bytes;
+    }
+    w.part = (float*)take(part);
+    w.factor_part[0] = (float*)take(4 * units * s->rank * s->d_in);
+    w.factor_part[1] = (float*)take(4 * units * s->rank * s->d_out);
+    w.at = (uint16_t*)take(2 * (size_t)s->n * s->rank * s->d_in);
+  }
   w.bytes = size_t(p - (char*)ws);
   return w;
 }
@@ -89,10 +138,11 @@ __global__ void clear_status_kernel(int32_t* status) { *status = 0; }
 
 // One workgroup: counts -> where each chunk's tokens of an adapter start within the adapter's rows, and the adapters' first rows.
 __global__ __launch_bounds__(1024) void scan_ids_kernel(int32_t* __restrict__ counts, int chunks, int n, int T, int32_t* __restrict__ first,
-                                                        int32_t* __restrict__ all) {
-  __shared__ int32_t waves[16];
+                                                        int32_t* __restrict__ all, int32_t* __restrict__ unit_first,
+                                                        int32_t* __restrict__ unit_adapter, int unit) {
+  __shared__ int32_t waves[16], unit_waves[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  int base = 0;
+  int base = 0, unit_base = 0;
   for (int a0 = 0; a0 <= n; a0 += 1024) {
     const int a = a0 + tid;
     int total = 0;
@@ -103,12 +153,29 @@ __global__ __launch_bounds__(1024) void scan_ids_kernel(int32_t* __restrict__ co
       total += here;
     }
     const int incl = lz::wave_scan(total, [](int x, int y) { return x + y; });
-    if (lane == 63) waves[wave] = incl;
+    // an adapter without tokens has a unit of no rows: its gradients are zeros
+    const int units = a < n && unit_first != nullptr ? (total > unit ? (total + unit - 1) / unit : 1) : 0;
+    const int unit_incl = lz::wave_scan(units, [](int x, int y) { return x + y; });
+    if (lane == 63) {
+      waves[wave] = incl;
+      unit_waves[wave] = unit_incl;
+    }
     __syncthreads();
-    int before = base;
-    for (int w = 0; w < wave; ++w) before += waves[w];
+    int before = base, unit_before = unit_base;
+    for (int w = 0; w < wave; ++w) {
+      before += waves[w];
+      unit_before += unit_waves[w];
+    }
     if (a <= n) first[a] = before + incl - total;
-    for (int w = 0; w < 16; ++w) base += waves[w];
+    if (a <= n && unit_first != nullptr) {
+      const int at = unit_before + unit_incl - units;
+      unit_first[a] = at;
+      for (int u = 0; u < units; ++u) unit_adapter[at + u] = a;
+    }
+    for (int w = 0; w < 16; ++w) {
+      base += waves[w];
+      unit_base += unit_waves[w];
+    }
     __syncthreads();
   }
   if (tid == 0) {
@@ -245,6 +312,100 @@ int32_t backward(const AdapterWorkspace& w, const lz_adapter_shape* s, const voi
   return rc;
 }
 
+// Tokens by adapter: w.order, w.row_of, w.first, and what the shape's kernels take their work from.
+int32_t sort_tokens(const AdapterWorkspace& w, const lz_adapter_shape* s, hipStream_t st, int32_t* status = nullptr, const int32_t* ids = nullptr) {
+  const int T = s->T, n = s->n, chunk = chunk_tokens(T), chunks = chunks_of(T);
+  const size_t lds = 4 * (size_t)(n + 1);
+  hipLaunchKernelGGL(count_ids_kernel, dim3(chunks), dim3(64), lds, st, ids ? ids : w.ids, T, n, chunk, w.ids, w.counts, status);
+  hipLaunchKernelGGL(scan_ids_kernel, dim3(1), dim3(1024), 0, st, w.counts, chunks, n, T, w.first, w.all, w.unit_first, w.unit_adapter,
+                     factor_chunk(T));
+  hipLaunchKernelGGL(place_ids_kernel, dim3(chunks), dim3(64), lds, st, w.ids, T, n, chunk, w.counts, w.first, w.order, w.row_of);
+  return lz::launch_status();
+}
+// ... for the kernels of every size
+int32_t sort_with_tables(const AdapterWorkspace& w, const lz_adapter_shape* s, hipStream_t st, int32_t* status = nullptr,
+                         const int32_t* ids = nullptr) {
+  int32_t rc = sort_tokens(w, s, st, status, ids);
+  if (rc != LZ_OK) return rc;
+  auto tables = [&](const int32_t* offsets, int S, void* rows, void* split) {
+    TileSpecs specs{};
+    add_rows(specs, kF32Rows, s->T, carve_tiles(rows, s->T, S, kF32Rows));
+    add_rows(specs, kSplitRows, s->T, carve_tiles(split, s->T, S, kSplitRows));
+    return launch_build_tiles(offsets, S, specs, st);
+  };
+  rc = tables(w.first, s->n, w.tiles, w.tiles_split);
+  return rc == LZ_OK ? tables(w.all, 1, w.all_tiles, w.all_tiles_split) : rc;
+}
+
+// ---- bf16 kernels
+
+// One token's rows are read by its own wave where tokens are few: an adapter after the other costs a workgroup of 16 a trip each.
+constexpr int kFewTokens = 128;
+
+int32_t low_rank_mfma(const AdapterWorkspace& w, const lz_adapter_shape* s, const void* x, int d, const void* a, const float* scale, void* h,
+                      hipStream_t st) {
+  const LowRankArgs args{(const uint16_t*)x, (const uint16_t*)a, scale, w.ids, w.lists.count64, w.lists.list64, w.lists.local64,
+                         (uint16_t*)h, s->T, d, s->rank};
+  if (s->T <= kFewTokens) hipLaunchKernelGGL(low_rank_token_kernel, dim3(s->T, ceil_div(s->rank, 4)), dim3(256), 0, st, args);
+  else if (s->T < 8192) hipLaunchKernelGGL((low_rank_kernel<1>), dim3(ceil_div(s->T, 16)), dim3(512), 0, st, args);
+  else hipLaunchKernelGGL((low_rank_kernel<2>), dim3(ceil_div(s->T, 32)), dim3(512), 0, st, args);
+  return lz::launch_status();
+}
+
+// out = A W + h b, or A W^T + h b^T
+template <int MODE>
+int32_t projection(const AdapterWorkspace& w, const lz_adapter_shape* s, const void* A, int K, const void* W, int n_out, const void* h,
+                   const void* b, void* out, hipStream_t st) {
+  if (narrow_tiles(s, n_out, K)) {
+    const AdapterNarrowArgs a{(const uint16_t*)A, (const uint16_t*)W, (uint16_t*)out, w.part, (const uint16_t*)h, (const uint16_t*)b,
+                              w.lists.count64, w.lists.list64, w.lists.local64, s->T, K, n_out, s->rank, s->n, ceil_div(n_out, kNarrow),
+                              splits_of(s, n_out, K)};
+    return launch_adapter_narrow<MODE>(a, st);
+  }
+  MfmaArgs a{};
+  a.A = (const uint16_t*)A;
+  a.W = (const uint16_t*)W;
+  a.C = (uint16_t*)out;
+  a.P = s->T;
+  a.K = K;
+  a.w_rows = n_out;
+  a.n_out = a.ldw = n_out;
+  a.n_tiles = ceil_div(n_out, BN);
+  a.adapter = AdapterSteps{(const uint16_t*)h, (const uint16_t*)b, w.lists.count256, w.lists.list256, w.lists.local256, s->rank};
+  return launch_mfma<EPI_ADAPTER, MODE>(a, st);
+}
+
+int32_t forward_mfma(const AdapterWorkspace& w, const lz_adapter_shape* s, const void* x, const void* W, const void* a, const void* b,
+                     const float* scale, void* h, void* y, hipStream_t st) {
+  const int32_t rc = low_rank_mfma(w, s, x, s->d_in, a, scale, h, st);
+  return rc == LZ_OK ? projection<MODE_NN>(w, s, x, s->d_in, W, s->d_out, h, b, y, st) : rc;
+}
+
+int32_t backward_mfma(const AdapterWorkspace& w, const lz_adapter_shape* s, const void* dy, const void* x, const void* h, const void* W,
+                      const void* a, const void* b, const float* scale, void* dx, void* da, void* db, hipStream_t st) {
+  int32_t rc = sort_tokens(w, s, st);
+  if (rc == LZ_OK) rc = low_rank_mfma(w, s, dy, s->d_out, b, scale, w.dh, st);
+  if (rc == LZ_OK) rc = lz_pack_weights(a, s->n, s->rank, s->d_in, LZ_BF16, w.at, st);  // its K steps lie along the rank
+  if (rc == LZ_OK) rc = projection<MODE_NT>(w, s, dy, s->d_out, W, s->d_in, w.dh, w.at, dx, st);
+  if (rc != LZ_OK) return rc;
+  FactorPair f{};
+  f.f[0] = FactorArgs{(const uint16_t*)w.dh, (const uint16_t*)x, (uint16_t*)da, w.factor_part[0], s->d_in, ceil_div(s->d_in, kFactorCols)};
+  f.f[1] = FactorArgs{(const uint16_t*)h, (const uint16_t*)dy, (uint16_t*)db, w.factor_part[1], s->d_out, ceil_div(s->d_out, kFactorCols)};
+  f.first = w.first, f.order = w.order, f.unit_first = w.unit_first, f.unit_adapter = w.unit_adapter;
+  f.n = s->n, f.rank = s->rank, f.rank_tiles = ceil_div(s->rank, 64), f.chunk = factor_chunk(s->T);
+  rc = allow_lds<factor_gradient_kernel>(kFactorLds);
+  if (rc != LZ_OK) return rc;
+  hipLaunchKernelGGL(factor_gradient_kernel, dim3(factor_units(s), (f.f[0].n_tiles + f.f[1].n_tiles) * f.rank_tiles), dim3(256), kFactorLds, st, f);
+  if (s->T > f.chunk) hipLaunchKernelGGL(join_factors_kernel, dim3(s->n, 2, 16), dim3(256), 0, st, f);
+  return lz::launch_status();
+}
+
+inline bool all16(std::initializer_list<const void*> tensors) {
+  for (const void* t : tensors)
+    if (!aligned16(t)) return false;
+  return true;
+}
+
 int32_t check(const lz_adapter_shape* s, void* ws, size_t ws_bytes, AdapterWorkspace* w) {
   if (!shape_ok(s)) return LZ_ESHAPE;
   *w = carve(ws, s);
@@ -265,23 +426,14 @@ extern "C" int32_t lz_adapter_plan(const int32_t* ids, const lz_adapter_shape* s
   if (rc != LZ_OK) return rc;
   hipStream_t st = (hipStream_t)stream;
   if (shape->T > 0 && !ids) return LZ_EINVAL;
-  if (status_opt) hipLaunchKernelGGL(clear_status_kernel, dim3(1), dim3(1), 0, st, status_opt);
+  // (one workgroup of the lists' kernel writes the word by itself)
+  if (status_opt && !(whole_pieces(shape) && shape->T > 0 && shape->T <= 256))
+    hipLaunchKernelGGL(clear_status_kernel, dim3(1), dim3(1), 0, st, status_opt);
   if (shape->T == 0) return lz::launch_status();
-  const int T = shape->T, n = shape->n, chunk = chunk_tokens(T), chunks = chunks_of(T);
-  const size_t lds = 4 * (size_t)(n + 1);
-  hipLaunchKernelGGL(count_ids_kernel, dim3(chunks), dim3(64), lds, st, ids, T, n, chunk, w.ids, w.counts, status_opt);
-  hipLaunchKernelGGL(scan_ids_kernel, dim3(1), dim3(1024), 0, st, w.counts, chunks, n, T, w.first, w.all);
-  hipLaunchKernelGGL(place_ids_kernel, dim3(chunks), dim3(64), lds, st, w.ids, T, n, chunk, w.counts, w.first, w.order, w.row_of);
-  rc = lz::launch_status();
-  if (rc != LZ_OK) return rc;
-  auto tables = [&](const int32_t* offsets, int S, void* rows, void* split) {
-    TileSpecs specs{};
-    add_rows(specs, kF32Rows, T, carve_tiles(rows, T, S, kF32Rows));
-    add_rows(specs, kSplitRows, T, carve_tiles(split, T, S, kSplitRows));
-    return launch_build_tiles(offsets, S, specs, st);
-  };
-  rc = tables(w.first, n, w.tiles, w.tiles_split);
-  return rc == LZ_OK ? tables(w.all, 1, w.all_tiles, w.all_tiles_split) : rc;
+  if (!whole_pieces(shape)) return sort_with_tables(w, shape, st, status_opt, ids);
+  hipLaunchKernelGGL(adapter_lists_kernel, dim3(ceil_div(shape->T, 256)), dim3(256), 4 * (size_t)shape->n, st, ids, shape->T, shape->n, w.ids,
+                     w.lists, status_opt);
+  return lz::launch_status();
 }
 
 extern "C" int32_t lz_adapter_forward(const void* x, const void* w, const void* a, const void* b, const float* scale,
@@ -291,6 +443,11 @@ extern "C" int32_t lz_adapter_forward(const void* x, const void* w, const void* 
   if (rc != LZ_OK || shape->T == 0) return rc;
   if (!x || !w || !a || !b || !scale || !h || !y) return LZ_EINVAL;
   hipStream_t st = (hipStream_t)stream;
+  if (whole_pieces(shape)) {
+    if (all16({x, w, a, b, h, y})) return forward_mfma(m, shape, x, w, a, b, scale, h, y, st);
+    const int32_t sorted = sort_with_tables(m, shape, st);
+    if (sorted != LZ_OK) return sorted;
+  }
   return shape->dtype == LZ_F32 ? forward<float>(m, shape, x, w, a, b, scale, h, y, st)
                                 : forward<uint16_t>(m, shape, x, w, a, b, scale, h, y, st);
 }
@@ -314,6 +471,11 @@ extern "C" int32_t lz_adapter_backward(const void* dy, const void* x, const void
     return lz::launch_status();
   }
   if (!dy || !x || !h || !w || !a || !b || !scale || !dx) return LZ_EINVAL;
+  if (whole_pieces(shape)) {
+    if (all16({dy, x, h, w, a, b, dx, da, db})) return backward_mfma(m, shape, dy, x, h, w, a, b, scale, dx, da, db, st);
+    const int32_t sorted = sort_with_tables(m, shape, st);
+    if (sorted != LZ_OK) return sorted;
+  }
   return shape->dtype == LZ_F32 ? backward<float>(m, shape, dy, x, h, w, a, b, scale, dx, da, db, st)
                                 : backward<uint16_t>(m, shape, dy, x, h, w, a, b, scale, dx, da, db, st);
 }

@@ -35,7 +35,8 @@ typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 // *_KEEP: the training forward; besides act(z) the pre-activation z goes to MfmaArgs::Z.
 // EPI_ACCUM: the result is added to the fp32 matrix MfmaArgs::Cacc (weight gradients summed over
 // micro-batches) instead of being stored as bf16.
-enum { EPI_NONE = 0, EPI_GELU = 1, EPI_SWIGLU = 2, EPI_GELU_KEEP = 3, EPI_SWIGLU_KEEP = 4, EPI_ACCUM = 5 };
+// EPI_ADAPTER: the K steps are followed by those of the low-rank adapters that a row tile's rows use (AdapterSteps).
+enum { EPI_NONE = 0, EPI_GELU = 1, EPI_SWIGLU = 2, EPI_GELU_KEEP = 3, EPI_SWIGLU_KEEP = 4, EPI_ACCUM = 5, EPI_ADAPTER = 8 };
 
 // ------------------------------------------------------------------------------------------
 // gfx950 MFMA kernel, bf16 in / fp32 accumulate / bf16 out
@@ -49,6 +50,17 @@ constexpr int kWStages = 3;
 constexpr int kLdsBytes = 2 * kATile + kWStages * kWTile;
 __device__ __forceinline__ constexpr int a_stage_off(int s) { return s * kATile; }
 __device__ __forceinline__ constexpr int w_stage_off(int w) { return 2 * kATile + w * kWTile; }
+
+// EPI_ADAPTER: C += h[row] B_a for the adapter a of every row.  A tile's rows use few adapters; each adds ceil(rank / 64) K steps,
+// whose left operand is h with the rows of other adapters read as zero and whose right one is the adapter's factor.
+struct AdapterSteps {
+  const uint16_t* h;      // [rows, rank]
+  const uint16_t* b;      // [n, rank, n_out], MODE_NT: [n, n_out, rank]
+  const int32_t* count;   // adapters of every row tile
+  const int32_t* list;    // [tile][BM] which
+  const uint8_t* local;   // [tile][BM] where in the list a row's adapter stands (none: past its end), row 8 (4 i + w) + l at 8 (8 w + l) + i
+  int rank;
+};
 
 struct MfmaArgs {
   const uint16_t* A;    // MODE_NT, MODE_NN: [P, K];  MODE_TN: [rows of the batch, lda]
@@ -74,6 +86,7 @@ struct MfmaArgs {
   const int32_t* gather;
   int gather_k;
   long long gather_T;
+  AdapterSteps adapter;
 };
 
 // stores of an epilogue's last pass (EPI_ACCUM: not the same in every wave)
@@ -199,6 +212,14 @@ struct Operands {
   int voffX[8], voffW[8];           // byte offsets of the loads of one stage
   int tail_or;                      // KTAIL: what the last K step ORs into them
   int no_row;                       // GATHER: bit i: load i's row lies past the tile's end
+  static constexpr bool kAdapter = EPI == EPI_ADAPTER;
+  int base_steps;                   // without the adapters'
+  const uint16_t *step_x, *step_w;  // EPI_ADAPTER: what the descriptors of the step that begin_step() named cover
+  uint32_t step_x_bytes, step_w_bytes;
+  int lane_row, lane_chunk;         // ... this lane's row of load 0, the 8 k of it that it loads
+  uint2 local;                      // ... where in the tile's list the adapters of its 8 rows stand
+  int rows, tile_index, col0;
+  int entry, entry_k;               // ... of the next step: which of the list's adapters, from which k on
 
   // ---- buffer descriptors: out-of-range loads return zero instead of faulting.  The activation
   // descriptor covers just this tile's rows, so 32-bit offsets do however large P is.
@@ -214,7 +235,8 @@ struct Operands {
   // piece l%32, which must hold logical piece (l%32) ^ swz_kmajor(k-row).
   __device__ __forceinline__ void set(const MfmaArgs& a, char* smem, const Tile& t) {
     if (t.slot < 0) {  // no tile: its loads have no bytes
-      k_steps = 0;
+      k_steps = base_steps = 0;
+      if constexpr (kAdapter) step_x_bytes = step_w_bytes = 0;
       a_bytes = w_bytes = 0;
       return;
     }
@@ -259,10 +281,24 @@ struct Operands {
       tileW = a.W + (size_t)t.slot * a.w_rows * K;
       w_extent = (uint32_t)((unsigned long long)a.w_rows * K * 2);
     }
-    k_steps = (K + BK - 1) / BK;
+    k_steps = base_steps = (K + BK - 1) / BK;
+    if constexpr (kAdapter) {
+      tile_index = t.row0 / BM;
+      col0 = t.n0;
+      entry = entry_k = 0;
+      rows = n_rows;
+      lane_row = wave * 8 + (lane >> 3);
+      lane_chunk = ((lane & 7) ^ swz(lane_row)) * 8;
+      local = *(const uint2*)(a.adapter.local + (size_t)tile_index * BM + lane_row * 8);
+      k_steps += ((const __attribute__((address_space(4))) int*)a.adapter.count)[tile_index] * ((a.adapter.rank + BK - 1) / BK);
+    }
     wordsA = rsrc_words(tileA, a_extent);
     wordsW = rsrc_words(tileW, w_extent);
     wordsNull = rsrc_words(a.A, 0);
+    if constexpr (kAdapter) {  // of the first two steps: the host sees to it that there are two
+      step_x = tileA, step_x_bytes = a_extent;
+      step_w = tileW, step_w_bytes = w_extent;
+    }
     no_row = 0;
     auto voff_kmajor = [&](int i, int ld, int col0) {
       const int kr = (i * 4 + wave) * 2 + (lane >> 5);
@@ -309,10 +345,71 @@ struct Operands {
     }
   }
 
+  // EPI_ADAPTER, before the loads of a step: its descriptors, and past the base's steps the offsets, whose former values no load
+  // needs any more.
+  __device__ __forceinline__ void begin_step(const MfmaArgs& a, int step) {
+    if constexpr (kAdapter) {
+      name_step(a, step);
+      // what the descriptors are made of stays in scalar registers, whichever branch it came from
+      auto scalar = [](const uint16_t* p) {
+        const uint64_t v = (uint64_t)p;
+        return (const uint16_t*)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v) |
+                                 (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32);
+      };
+      step_x = scalar(step_x), step_w = scalar(step_w);
+      step_x_bytes = __builtin_amdgcn_readfirstlane((int)step_x_bytes), step_w_bytes = __builtin_amdgcn_readfirstlane((int)step_w_bytes);
+    }
+  }
+  __device__ __forceinline__ void name_step(const MfmaArgs& a, int step) {
+    if constexpr (kAdapter) {
+      if (step < base_steps) {
+        step_x = tileA, step_x_bytes = a_extent;
+        step_w = tileW, step_w_bytes = w_extent;
+        return;
+      }
+      if (step >= k_steps) {
+        step_x_bytes = step_w_bytes = 0;
+        return;
+      }
+      const int rank = a.adapter.rank, e = entry, k0 = entry_k;  // (step - base_steps, divided: by the vector unit, whose results
+      entry_k += BK;                                             // no descriptor can be made of)
+      if (entry_k >= rank) {
+        entry_k = 0;
+        ++entry;
+      }
+      const int id = ((const __attribute__((address_space(4))) int*)a.adapter.list)[(size_t)tile_index * BM + e];
+      const int row0 = tile_index * BM;
+      step_x = a.adapter.h + (size_t)row0 * rank, step_x_bytes = (uint32_t)rows * (uint32_t)rank * 2u;
+      const uint16_t* const b = a.adapter.b + (size_t)id * rank * a.n_out;
+      const bool in = k0 + lane_chunk < rank;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const bool mine = in && (((i < 4 ? local.x : local.y) >> (8 * (i & 3))) & 255u) == (unsigned)e;
+        voffX[i] = mine ? ((lane_row + 32 * i) * rank + k0 + lane_chunk) * 2 : (int)0x80000000;
+      }
+      if constexpr (TB) {  // k-rows past the rank lie past the descriptor
+        step_w = b + (size_t)k0 * a.n_out, step_w_bytes = (uint32_t)(rank - k0) * (uint32_t)a.n_out * 2u;
+      } else {
+        step_w = b, step_w_bytes = (uint32_t)rank * (uint32_t)a.n_out * 2u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) voffW[i] = in ? ((col0 + lane_row + 32 * i) * rank + k0 + lane_chunk) * 2 : (int)0x80000000;
+      }
+    }
+  }
+  // EPI_ADAPTER: the list's places have arrived: the compiler waits for them here, ahead of the loads of a K loop, whose number it
+  // does not know.
+  __device__ __forceinline__ void settle() {
+    if constexpr (kAdapter) asm volatile("" : "+v"(local.x), "+v"(local.y));
+  }
+  // Bytes a step lies past the tile's first.
+  __device__ __forceinline__ int soffset(int step, int bytes) const { return kAdapter && step >= base_steps ? 0 : step * bytes; }
+
   // The descriptors for K step `step`.  A step past the end of K is "loaded" through a zero-length one: no memory traffic.
   __device__ __forceinline__ i32x4 words_x(int step) const {
     const bool real = step < k_steps;
-    if constexpr (MODE == MODE_TN) {
+    if constexpr (kAdapter) {
+      return rsrc_words(step_x, step_x_bytes);
+    } else if constexpr (MODE == MODE_TN) {
       // bytes left of the slot: a step that begins inside the slot begins inside both extents (the
       // tile's first column lies inside the operand's row)
       const uint32_t off = (uint32_t)step * (uint32_t)stepA64;
@@ -326,7 +423,9 @@ struct Operands {
   }
   __device__ __forceinline__ i32x4 words_w(int step) const {
     const bool real = step < k_steps;
-    if constexpr (MODE == MODE_TN) {
+    if constexpr (kAdapter) {
+      return rsrc_words(step_w, step_w_bytes);
+    } else if constexpr (MODE == MODE_TN) {
       const uint32_t off = (uint32_t)step * (uint32_t)stepW64;
       return rsrc_words((const char*)tileW + off, real ? w_extent - off : 0u);
     } else if constexpr (MODE == MODE_TN_WIDE) {
@@ -341,18 +440,18 @@ struct Operands {
   __device__ __forceinline__ void load_x(int stage, int step, int i, const i32x4& words, f32x4* with_mfma = nullptr,
                                          const bf16x8* mw = nullptr, const bf16x8* mx = nullptr) const {
     int voff = voffX[i];
-    if constexpr (KTAIL && !TA) voff |= tail_or & (step == k_steps - 1 ? -1 : 0);
+    if constexpr (KTAIL && !TA) voff |= tail_or & (step == base_steps - 1 ? -1 : 0);
     const uint32_t to = lds + a_stage_off(stage) + i * 4096;
-    if (with_mfma != nullptr) mfma_then_load16_to_lds(*with_mfma, *mw, *mx, words, to, voff, step * stepA);
-    else load16_to_lds(words, to, voff, step * stepA);
+    if (with_mfma != nullptr) mfma_then_load16_to_lds(*with_mfma, *mw, *mx, words, to, voff, soffset(step, stepA));
+    else load16_to_lds(words, to, voff, soffset(step, stepA));
   }
   __device__ __forceinline__ void load_w(int stage, int step, int i, const i32x4& words, f32x4* with_mfma = nullptr,
                                          const bf16x8* mw = nullptr, const bf16x8* mx = nullptr) const {
     int voff = voffW[i];
-    if constexpr (KTAIL && !TB) voff |= tail_or & (step == k_steps - 1 ? -1 : 0);
+    if constexpr (KTAIL && !TB) voff |= tail_or & (step == base_steps - 1 ? -1 : 0);
     const uint32_t to = lds + w_stage_off(stage) + i * 4096;
-    if (with_mfma != nullptr) mfma_then_load16_to_lds(*with_mfma, *mw, *mx, words, to, voff, step * stepW);
-    else load16_to_lds(words, to, voff, step * stepW);
+    if (with_mfma != nullptr) mfma_then_load16_to_lds(*with_mfma, *mw, *mx, words, to, voff, soffset(step, stepW));
+    else load16_to_lds(words, to, voff, soffset(step, stepW));
   }
   // GATHER: pairs to offsets
   __device__ __forceinline__ void gather_rows(const MfmaArgs& a) {
@@ -545,6 +644,42 @@ struct Draws {
   }
 };
 
+// Tiles that are as many for every workgroup and cost the same: no queue, no table.  Each XCD has a run of the tiles, in bands of kGroupM row
+// tiles, columns of a band one after the other: what an XCD works on at a time are kGroupM x 8 tiles that share panels.
+struct FixedDraws {
+  const MfmaArgs& a;
+  int at, end;  // this workgroup's tile, the XCD's last
+  __device__ __forceinline__ FixedDraws(const MfmaArgs& args, char*) : a(args) {
+    const int xcd = blockIdx.x % 8;
+    const long long tiles = (long long)((a.P + BM - 1) / BM) * a.n_tiles;
+    at = int(tiles * xcd / 8) + (int)(blockIdx.x / 8);
+    end = int(tiles * (xcd + 1) / 8);
+  }
+  __device__ __forceinline__ void request() {}
+  __device__ __forceinline__ void publish(char*) {}
+  __device__ __forceinline__ void receive(const char*) {
+    __syncthreads();
+    at += gridDim.x / 8;
+  }
+  __device__ __forceinline__ void finish() {}
+  __device__ __forceinline__ Tile tile(int n_out_cols) const {
+    if (at >= end) return Tile{-1, 0, 0, 0, 0, 0, 0};
+    const int m_tiles = int((a.P + BM - 1) / BM), band = at / (kGroupM * a.n_tiles), within = at - band * kGroupM * a.n_tiles;
+    const int left = m_tiles - band * kGroupM, nr = left < kGroupM ? left : kGroupM, col = within / nr;
+    const int row0 = (band * kGroupM + within - col * nr) * BM;
+    return Tile{0, row0, a.P - row0 < BM ? (int)a.P : row0 + BM, col * n_out_cols, 0, 0, 0};
+  }
+};
+template <int EPI>
+constexpr bool kFixed = EPI == EPI_ADAPTER;
+template <int EPI, bool PAIR>
+using DrawsOf = typename std::conditional<kFixed<EPI>, FixedDraws, Draws<PAIR>>::type;
+template <int EPI, bool PAIR>
+__device__ __forceinline__ DrawsOf<EPI, PAIR> first_draw(const MfmaArgs* args, char* smem) {
+  if constexpr (kFixed<EPI>) return FixedDraws(args[0], smem);
+  else return Draws<PAIR>(args[0].u, args[PAIR ? 1 : 0].u, smem);
+}
+
 template <int EPI>
 constexpr int kOutCols = (EPI == EPI_SWIGLU || EPI == EPI_SWIGLU_KEEP) ? BN / 2 : BN;
 
@@ -556,7 +691,7 @@ constexpr int kOutCols = (EPI == EPI_SWIGLU || EPI == EPI_SWIGLU_KEEP) ? BN / 2 
 // go to ops and its first loads out within the epilogue.
 template <int EPI, int XF, int MODE, bool GATHER, bool KTAIL, bool PAIR>
 __device__ __forceinline__ Tile gemm_tile(const MfmaArgs* args, char* smem, const Tile tile, Operands<EPI, MODE, GATHER, KTAIL>& ops,
-                                          Draws<PAIR>& draws) {
+                                          DrawsOf<EPI, PAIR>& draws) {
   const MfmaArgs& a = args[PAIR ? __builtin_amdgcn_readfirstlane(tile.part) : 0];
   constexpr bool TA = MODE == MODE_TN || MODE == MODE_TN_WIDE, TB = MODE != MODE_NT;  // k-major left / right operand
   constexpr bool kGated = EPI == EPI_SWIGLU || EPI == EPI_SWIGLU_KEEP;
@@ -728,6 +863,7 @@ __device__ __forceinline__ Tile gemm_tile(const MfmaArgs* args, char* smem, cons
   auto k_step = [&](int kt, auto as_c, auto wst_c) {
     constexpr int as = decltype(as_c)::value, wst = decltype(wst_c)::value;
     constexpr int as_next = as ^ 1, wst_next = (wst + 1) % D, wst_prev = (wst + D - 1) % D;
+    ops.begin_step(a, kt + 2);  // of both operands: D = 3
     // unit (0, 0) runs; weight fragments of (0, 1), first half of slice 1's activation fragments
     unit(0, 0, 0, wst, 0, 1, 1, as, 1, 1, 0, kHalf, false, as_next, kt + 1, wst_prev, kt - 1 + D, kAfterBarrier, kL1);
     // unit (0, 1) runs; weight fragments of (1, 0), the rest of slice 1's activation fragments
@@ -799,14 +935,17 @@ __device__ __forceinline__ Tile gemm_tile(const MfmaArgs* args, char* smem, cons
   constexpr int kPerRows = EPI == EPI_SWIGLU_KEEP ? 3 : EPI == EPI_GELU_KEEP ? 2 : 1;  // passes over the same 32 rows
   constexpr int kPasses = EPI == EPI_ACCUM ? 2 * XF : XF * kPerRows;
   constexpr int kFeedPasses = kPasses < 2 ? 1 : 2, kFeed0 = kPasses - kFeedPasses;
-  constexpr int kTurn = kFeed0 - (GATHER && kFeed0 > 0 ? 1 : 0);
+  constexpr int kTurn = kFeed0 - ((GATHER || EPI == EPI_ADAPTER) && kFeed0 > 0 ? 1 : 0);
   Tile next;
   auto begin_pass = [&](int p) {
     if (p == kTurn) {
       next = draws.tile(kOutCols<EPI>);
       ops.set(args[PAIR ? __builtin_amdgcn_readfirstlane(next.part) : 0], smem, next);
     }
-    if (p == kFeed0) ops.gather_rows(args[0]);
+    if (p == kFeed0) {
+      ops.gather_rows(args[0]);
+      ops.settle();
+    }
     __builtin_amdgcn_sched_barrier(0);
   };
   // after cell c of n of pass p's writes
@@ -959,11 +1098,12 @@ __global__ __launch_bounds__(256, 1) void gemm_mfma_kernel(MfmaLaunch<PAIR> laun
 #if defined(__HIP_DEVICE_COMPILE__)  // the host pass only needs the launch stub, not the gfx950 builtins
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const MfmaArgs* const args = launch.gemm;
-  Draws<PAIR> draws(args[0].u, args[PAIR ? 1 : 0].u, smem);
+  DrawsOf<EPI, PAIR> draws = first_draw<EPI, PAIR>(args, smem);
   Tile tile = draws.tile(kOutCols<EPI>);
   Operands<EPI, MODE, GATHER, KTAIL> ops;
   ops.set(args[PAIR ? __builtin_amdgcn_readfirstlane(tile.part) : 0], smem, tile);
   ops.gather_rows(args[0]);
+  ops.settle();
   if (tile.slot >= 0) {
 #pragma unroll
     for (int l = 0; l < kFirstLoads; ++l) ops.load_first(l);

@@ -60,6 +60,21 @@ def test_forward_and_gradients(case, dtype):
     _run(case, dtype, 11)
 
 
+# as many tiles as the wide kernel takes, in one direction or both; tiles of one adapter, of a few and of as many as rows
+WIDE = [
+    (6100, 136, 1032, 16, 5, 9, 0.1),
+    (6000, 1032, 136, 72, 3, 4, 0.0),
+    (2600, 1288, 1416, 24, 300, 2600, 0.3),
+    (6145, 320, 1096, 8, 4000, 6145, 0.0),
+    (3000, 1100 // 8 * 8, 2056, 128, 2, 1, 0.0),
+]
+
+
+@pytest.mark.parametrize("case", WIDE, ids=lambda c: "x".join(str(v) for v in c[:5]))
+def test_many_tiles(case):
+    _run(case, BF16, 13)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
 def test_no_token_has_an_adapter(dtype):
     case = (130, 256, 128, 16, 3, 1, 0.0)
