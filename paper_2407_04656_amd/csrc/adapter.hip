@@ -367,6 +367,8 @@ int32_t projection(const AdapterWorkspace& w, const lz_adapter_shape* s, const v
   a.W = (const uint16_t*)W;
   a.C = (uint16_t*)out;
   a.P = s->T;
+  a.matrices = 1;
+  a.rows_each = s->T;
   a.K = K;
   a.w_rows = n_out;
   a.n_out = a.ldw = n_out;

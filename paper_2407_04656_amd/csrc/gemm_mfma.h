@@ -36,7 +36,17 @@ typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 // EPI_ACCUM: the result is added to the fp32 matrix MfmaArgs::Cacc (weight gradients summed over
 // micro-batches) instead of being stored as bf16.
 // EPI_ADAPTER: the K steps are followed by those of the low-rank adapters that a row tile's rows use (AdapterSteps).
-enum { EPI_NONE = 0, EPI_GELU = 1, EPI_SWIGLU = 2, EPI_GELU_KEEP = 3, EPI_SWIGLU_KEEP = 4, EPI_ACCUM = 5, EPI_ADAPTER = 8 };
+enum { EPI_NONE = 0, EPI_GELU = 1, EPI_SWIGLU = 2, EPI_GELU_KEEP = 3, EPI_SWIGLU_KEEP = 4, EPI_ACCUM = 5, EPI_ADAPTER = 8,
+// Products of orthogonalised updates (gemm_orthogonal.h): fp16 operands, in one plane or two, of equal matrices one behind the other.
+       EPI_GRAM = 9, EPI_GRAM_TWO = 10, EPI_SQUARE = 11, EPI_SQUARE_TWO = 12, EPI_APPLY = 13, EPI_APPLY_TWO = 14 };
+template <int EPI>
+constexpr bool kOrtho = EPI >= EPI_GRAM && EPI <= EPI_APPLY_TWO;
+template <int EPI>
+constexpr bool kTwoPlanes = EPI == EPI_GRAM_TWO || EPI == EPI_SQUARE_TWO || EPI == EPI_APPLY_TWO;
+template <int EPI>
+constexpr bool kApply = EPI == EPI_APPLY || EPI == EPI_APPLY_TWO;
+template <int EPI>  // only tiles on and below the diagonal, stored twice
+constexpr bool kSymmetric = kOrtho<EPI> && !kApply<EPI>;
 
 // ------------------------------------------------------------------------------------------
 // gfx950 MFMA kernel, bf16 in / fp32 accumulate / bf16 out
@@ -60,6 +70,15 @@ struct AdapterSteps {
   const int32_t* list;    // [tile][BM] which
   const uint8_t* local;   // [tile][BM] where in the list a row's adapter stands (none: past its end), row 8 (4 i + w) + l at 8 (8 w + l) + i
   int rank;
+};
+
+// kOrtho: C = factor sum + (symmetric) what belongs on the diagonal, or + rho X.
+struct OrthoProduct {
+  size_t plane_a, plane_w, plane_c;  // elements between the planes
+  float factor;
+  float on_diagonal;   // GRAM, SQUARE: added to the diagonal's sums
+  float* residual;     // one plane: what rounding takes from the diagonal of GRAM's result, [matrices][rows]; SQUARE adds 2 residual H
+  float rho;           // APPLY: X is W
 };
 
 struct MfmaArgs {
@@ -87,11 +106,14 @@ struct MfmaArgs {
   int gather_k;
   long long gather_T;
   AdapterSteps adapter;
+  // EPI_ADAPTER, kOrtho: equal matrices of so many rows each
+  int matrices, rows_each;
+  OrthoProduct ortho;
 };
 
 // stores of an epilogue's last pass (EPI_ACCUM: not the same in every wave)
 template <int EPI>
-constexpr int kLastStores = EPI == EPI_ACCUM ? 0 : EPI == EPI_SWIGLU || EPI == EPI_SWIGLU_KEEP ? 4 : 8;
+constexpr int kLastStores = EPI == EPI_APPLY_TWO ? 16 : EPI == EPI_ACCUM ? 0 : EPI == EPI_SWIGLU || EPI == EPI_SWIGLU_KEEP ? 4 : 8;
 
 // Operand layouts of the contraction C[m, n] = sum_k A(m, k) W(n, k):
 //   MODE_NT  A [m, k], W [n, k]: both contiguous along k (the data gradients)
@@ -127,8 +149,16 @@ __device__ __forceinline__ void load16_to_lds(i32x4 rsrc, uint32_t lds_base, int
 
 // The same load with an MFMA between the write of M0 and the load: the MFMA stands in for the wait
 // state the hardware wants there, and the three instructions fit the gap between two MFMAs.
+template <bool HALF>
 __device__ __forceinline__ void mfma_then_load16_to_lds(f32x4& acc, const bf16x8& w, const bf16x8& x, i32x4 rsrc,
                                                         uint32_t lds_base, int voffset, int soffset) {
+  if constexpr (HALF) {
+    asm volatile("s_mov_b32 m0, %3\n\tv_mfma_f32_16x16x32_f16 %0, %1, %2, %0\n\tbuffer_load_dwordx4 %4, %5, %6 offen lds"
+                 : "+a"(acc)
+                 : "v"(w), "v"(x), "s"(lds_base), "v"(voffset), "s"(rsrc), "s"(soffset)
+                 : "memory");
+    return;
+  }
   asm volatile("s_mov_b32 m0, %3\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0\n\tbuffer_load_dwordx4 %4, %5, %6 offen lds"
                : "+a"(acc)
                : "v"(w), "v"(x), "s"(lds_base), "v"(voffset), "s"(rsrc), "s"(soffset)
@@ -164,6 +194,12 @@ __device__ __forceinline__ float gelu_fast(float v) {
 // Two fp32 -> one dword of two bf16, round to nearest even (v_cvt_pk_bf16_f32 on gfx950).
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+  return __builtin_bit_cast(uint32_t, f16x2{(_Float16)lo, (_Float16)hi});
+}
+// (by value: a bit cast of a vector's element takes the vector's first)
+__device__ __forceinline__ f16x2 unpack_f16x2(uint32_t v) { return __builtin_bit_cast(f16x2, v); }
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   const f32x2 v = {lo, hi};
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
@@ -214,12 +250,15 @@ struct Operands {
   int no_row;                       // GATHER: bit i: load i's row lies past the tile's end
   static constexpr bool kAdapter = EPI == EPI_ADAPTER;
   int base_steps;                   // without the adapters'
-  const uint16_t *step_x, *step_w;  // EPI_ADAPTER: what the descriptors of the step that begin_step() named cover
+  static constexpr bool kNamed = kAdapter || kTwoPlanes<EPI>;
+  const uint16_t *step_x, *step_w;  // kNamed: what the descriptors of the step that begin_step() named cover
   uint32_t step_x_bytes, step_w_bytes;
   int lane_row, lane_chunk;         // ... this lane's row of load 0, the 8 k of it that it loads
   uint2 local;                      // ... where in the tile's list the adapters of its 8 rows stand
   int rows, tile_index, col0;
   int entry, entry_k;               // ... of the next step: which of the list's adapters, from which k on
+  int pair_step0;                   // kTwoPlanes: the first step of the pair of planes that begin_step() named
+  size_t plane_a, plane_w;
 
   // ---- buffer descriptors: out-of-range loads return zero instead of faulting.  The activation
   // descriptor covers just this tile's rows, so 32-bit offsets do however large P is.
@@ -236,7 +275,7 @@ struct Operands {
   __device__ __forceinline__ void set(const MfmaArgs& a, char* smem, const Tile& t) {
     if (t.slot < 0) {  // no tile: its loads have no bytes
       k_steps = base_steps = 0;
-      if constexpr (kAdapter) step_x_bytes = step_w_bytes = 0;
+      if constexpr (kNamed) step_x_bytes = step_w_bytes = 0;
       a_bytes = w_bytes = 0;
       return;
     }
@@ -295,7 +334,12 @@ struct Operands {
     wordsA = rsrc_words(tileA, a_extent);
     wordsW = rsrc_words(tileW, w_extent);
     wordsNull = rsrc_words(a.A, 0);
-    if constexpr (kAdapter) {  // of the first two steps: the host sees to it that there are two
+    if constexpr (kTwoPlanes<EPI>) {  // hi hi, hi lo, lo hi
+      k_steps = 3 * base_steps;
+      pair_step0 = 0;
+      plane_a = a.ortho.plane_a, plane_w = a.ortho.plane_w;
+    }
+    if constexpr (kNamed) {  // of the first two steps: the host sees to it that there are two
       step_x = tileA, step_x_bytes = a_extent;
       step_w = tileW, step_w_bytes = w_extent;
     }
@@ -348,7 +392,7 @@ struct Operands {
   // EPI_ADAPTER, before the loads of a step: its descriptors, and past the base's steps the offsets, whose former values no load
   // needs any more.
   __device__ __forceinline__ void begin_step(const MfmaArgs& a, int step) {
-    if constexpr (kAdapter) {
+    if constexpr (kNamed) {
       name_step(a, step);
       // what the descriptors are made of stays in scalar registers, whichever branch it came from
       auto scalar = [](const uint16_t* p) {
@@ -361,7 +405,14 @@ struct Operands {
     }
   }
   __device__ __forceinline__ void name_step(const MfmaArgs& a, int step) {
-    if constexpr (kAdapter) {
+    if constexpr (kTwoPlanes<EPI>) {
+      const bool second = step >= base_steps, third = step >= 2 * base_steps;
+      pair_step0 = third ? 2 * base_steps : second ? base_steps : 0;
+      step_x = tileA + (third ? plane_a : 0);
+      step_w = tileW + (second && !third ? plane_w : 0);
+      step_x_bytes = step < k_steps ? a_extent : 0;
+      step_w_bytes = step < k_steps ? w_extent : 0;
+    } else if constexpr (kAdapter) {
       if (step < base_steps) {
         step_x = tileA, step_x_bytes = a_extent;
         step_w = tileW, step_w_bytes = w_extent;
@@ -402,12 +453,15 @@ struct Operands {
     if constexpr (kAdapter) asm volatile("" : "+v"(local.x), "+v"(local.y));
   }
   // Bytes a step lies past the tile's first.
-  __device__ __forceinline__ int soffset(int step, int bytes) const { return kAdapter && step >= base_steps ? 0 : step * bytes; }
+  __device__ __forceinline__ int soffset(int step, int bytes) const {
+    if constexpr (kTwoPlanes<EPI>) return (step - pair_step0) * bytes;
+    return kAdapter && step >= base_steps ? 0 : step * bytes;
+  }
 
   // The descriptors for K step `step`.  A step past the end of K is "loaded" through a zero-length one: no memory traffic.
   __device__ __forceinline__ i32x4 words_x(int step) const {
     const bool real = step < k_steps;
-    if constexpr (kAdapter) {
+    if constexpr (kNamed) {
       return rsrc_words(step_x, step_x_bytes);
     } else if constexpr (MODE == MODE_TN) {
       // bytes left of the slot: a step that begins inside the slot begins inside both extents (the
@@ -423,7 +477,7 @@ struct Operands {
   }
   __device__ __forceinline__ i32x4 words_w(int step) const {
     const bool real = step < k_steps;
-    if constexpr (kAdapter) {
+    if constexpr (kNamed) {
       return rsrc_words(step_w, step_w_bytes);
     } else if constexpr (MODE == MODE_TN) {
       const uint32_t off = (uint32_t)step * (uint32_t)stepW64;
@@ -442,7 +496,7 @@ struct Operands {
     int voff = voffX[i];
     if constexpr (KTAIL && !TA) voff |= tail_or & (step == base_steps - 1 ? -1 : 0);
     const uint32_t to = lds + a_stage_off(stage) + i * 4096;
-    if (with_mfma != nullptr) mfma_then_load16_to_lds(*with_mfma, *mw, *mx, words, to, voff, soffset(step, stepA));
+    if (with_mfma != nullptr) mfma_then_load16_to_lds<kOrtho<EPI>>(*with_mfma, *mw, *mx, words, to, voff, soffset(step, stepA));
     else load16_to_lds(words, to, voff, soffset(step, stepA));
   }
   __device__ __forceinline__ void load_w(int stage, int step, int i, const i32x4& words, f32x4* with_mfma = nullptr,
@@ -450,7 +504,7 @@ struct Operands {
     int voff = voffW[i];
     if constexpr (KTAIL && !TB) voff |= tail_or & (step == base_steps - 1 ? -1 : 0);
     const uint32_t to = lds + w_stage_off(stage) + i * 4096;
-    if (with_mfma != nullptr) mfma_then_load16_to_lds(*with_mfma, *mw, *mx, words, to, voff, soffset(step, stepW));
+    if (with_mfma != nullptr) mfma_then_load16_to_lds<kOrtho<EPI>>(*with_mfma, *mw, *mx, words, to, voff, soffset(step, stepW));
     else load16_to_lds(words, to, voff, soffset(step, stepW));
   }
   // GATHER: pairs to offsets
@@ -644,14 +698,18 @@ struct Draws {
   }
 };
 
-// Tiles that are as many for every workgroup and cost the same: no queue, no table.  Each XCD has a run of the tiles, in bands of kGroupM row
-// tiles, columns of a band one after the other: what an XCD works on at a time are kGroupM x 8 tiles that share panels.
+// Tiles that cost the same, of equal matrices: no queue, no table.  Each XCD has a run of the tiles, in bands of kGroupM row tiles,
+// the columns of a band one after the other: what an XCD works on at a time are kGroupM x 8 tiles that share panels.
+template <bool SYMMETRIC>
 struct FixedDraws {
   const MfmaArgs& a;
-  int at, end;  // this workgroup's tile, the XCD's last
+  int at, end;             // this workgroup's tile, the XCD's last
+  int m_tiles, each;       // row tiles and tiles of a matrix
   __device__ __forceinline__ FixedDraws(const MfmaArgs& args, char*) : a(args) {
     const int xcd = blockIdx.x % 8;
-    const long long tiles = (long long)((a.P + BM - 1) / BM) * a.n_tiles;
+    m_tiles = (a.rows_each + BM - 1) / BM;
+    each = SYMMETRIC ? m_tiles * (m_tiles + 1) / 2 : m_tiles * a.n_tiles;
+    const long long tiles = (long long)a.matrices * each;
     at = int(tiles * xcd / 8) + (int)(blockIdx.x / 8);
     end = int(tiles * (xcd + 1) / 8);
   }
@@ -664,19 +722,40 @@ struct FixedDraws {
   __device__ __forceinline__ void finish() {}
   __device__ __forceinline__ Tile tile(int n_out_cols) const {
     if (at >= end) return Tile{-1, 0, 0, 0, 0, 0, 0};
-    const int m_tiles = int((a.P + BM - 1) / BM), band = at / (kGroupM * a.n_tiles), within = at - band * kGroupM * a.n_tiles;
-    const int left = m_tiles - band * kGroupM, nr = left < kGroupM ? left : kGroupM, col = within / nr;
-    const int row0 = (band * kGroupM + within - col * nr) * BM;
-    return Tile{0, row0, a.P - row0 < BM ? (int)a.P : row0 + BM, col * n_out_cols, 0, 0, 0};
+    const int matrix = at / each, t = at - matrix * each;
+    int row, col;
+    if constexpr (SYMMETRIC) {  // rows of a band: 8 b^2 + 2 b tiles lie above band b
+      int b = 0;
+      while (8 * (b + 1) * (b + 1) + 2 * (b + 1) <= t) ++b;
+      const int left = m_tiles - b * kGroupM, nr = left < kGroupM ? left : kGroupM, within = t - (8 * b * b + 2 * b);
+      if (within < kGroupM * b * nr) {
+        col = within / nr;
+        row = b * kGroupM + within - col * nr;
+      } else {  // the band's triangle
+        int w = within - kGroupM * b * nr, j = 0;
+        for (; w >= nr - j; ++j) w -= nr - j;
+        col = b * kGroupM + j;
+        row = col + w;
+      }
+    } else {
+      const int band = t / (kGroupM * a.n_tiles), within = t - band * kGroupM * a.n_tiles;
+      const int left = m_tiles - band * kGroupM, nr = left < kGroupM ? left : kGroupM;
+      col = within / nr;
+      row = band * kGroupM + within - col * nr;
+    }
+    // (divided by the vector unit: back to scalar registers, where descriptors are made)
+    auto scalar = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    const int slot = scalar(matrix), row0 = scalar(slot * a.rows_each + row * BM), row_end = (slot + 1) * a.rows_each;
+    return Tile{slot, row0, row_end - row0 < BM ? row_end : row0 + BM, scalar(col * n_out_cols), 0, 0, 0};
   }
 };
 template <int EPI>
-constexpr bool kFixed = EPI == EPI_ADAPTER;
+constexpr bool kFixed = EPI == EPI_ADAPTER || kOrtho<EPI>;
 template <int EPI, bool PAIR>
-using DrawsOf = typename std::conditional<kFixed<EPI>, FixedDraws, Draws<PAIR>>::type;
+using DrawsOf = typename std::conditional<kFixed<EPI>, FixedDraws<kSymmetric<EPI>>, Draws<PAIR>>::type;
 template <int EPI, bool PAIR>
 __device__ __forceinline__ DrawsOf<EPI, PAIR> first_draw(const MfmaArgs* args, char* smem) {
-  if constexpr (kFixed<EPI>) return FixedDraws(args[0], smem);
+  if constexpr (kFixed<EPI>) return FixedDraws<kSymmetric<EPI>>(args[0], smem);
   else return Draws<PAIR>(args[0].u, args[PAIR ? 1 : 0].u, smem);
 }
 
@@ -834,9 +913,15 @@ __device__ __forceinline__ Tile gemm_tile(const MfmaArgs* args, char* smem, cons
               &xf[xset][m % NA]);
       } else {
         issue(ld_a_stage, ld_a_step, ld_w_stage, ld_w_step, l0, l1);
-        asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0"
-                     : "+a"(acc[4 * hw + m / NA][m % NA])
-                     : "v"(wf[ws][m / NA]), "v"(xf[xset][m % NA]));
+        if constexpr (kOrtho<EPI>) {
+          asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0"
+                       : "+a"(acc[4 * hw + m / NA][m % NA])
+                       : "v"(wf[ws][m / NA]), "v"(xf[xset][m % NA]));
+        } else {
+          asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0"
+                       : "+a"(acc[4 * hw + m / NA][m % NA])
+                       : "v"(wf[ws][m / NA]), "v"(xf[xset][m % NA]));
+        }
       }
     }
   };
@@ -932,8 +1017,8 @@ __device__ __forceinline__ Tile gemm_tile(const MfmaArgs* args, char* smem, cons
   const int quad = lane >> 4;
   // Before pass kTurn of kPasses the next tile is looked up, and its first loads go out one by one within the writes to the
   // patch of the last two passes (a burst of 32 holds the wave for 2600 to 4700 cycles, until the texture unit has taken it).
-  constexpr int kPerRows = EPI == EPI_SWIGLU_KEEP ? 3 : EPI == EPI_GELU_KEEP ? 2 : 1;  // passes over the same 32 rows
-  constexpr int kPasses = EPI == EPI_ACCUM ? 2 * XF : XF * kPerRows;
+  constexpr int kPerRows = EPI == EPI_SWIGLU_KEEP ? 3 : EPI == EPI_GELU_KEEP ? 2 : kSymmetric<EPI> ? (kTwoPlanes<EPI> ? 4 : 2) : 1;  // passes over the same 32 rows
+  constexpr int kPasses = EPI == EPI_ACCUM || kApply<EPI> ? 2 * XF : XF * kPerRows;
   constexpr int kFeedPasses = kPasses < 2 ? 1 : 2, kFeed0 = kPasses - kFeedPasses;
   constexpr int kTurn = kFeed0 - ((GATHER || EPI == EPI_ADAPTER) && kFeed0 > 0 ? 1 : 0);
   Tile next;
@@ -978,8 +1063,13 @@ __device__ __forceinline__ Tile gemm_tile(const MfmaArgs* args, char* smem, cons
 #pragma unroll
       for (int c = 0; c < kWaveCols / 16; ++c) {
         uint2 pk;
-        pk.x = pack_bf16x2(value(c, h, 0), value(c, h, 1));
-        pk.y = pack_bf16x2(value(c, h, 2), value(c, h, 3));
+        if constexpr (kOrtho<EPI>) {
+          pk.x = pack_f16x2(value(c, h, 0), value(c, h, 1));
+          pk.y = pack_f16x2(value(c, h, 2), value(c, h, 3));
+        } else {
+          pk.x = pack_bf16x2(value(c, h, 0), value(c, h, 1));
+          pk.y = pack_bf16x2(value(c, h, 2), value(c, h, 3));
+        }
         *(uint2*)(patch + r * kPitch + ((((2 * c) | (quad >> 1)) ^ (r & (kLanesPerRow - 1))) << 4) + (quad & 1) * 8) = pk;
         feed(p, h * (kWaveCols / 16) + c, kWaveCols / 8);
       }
@@ -1047,6 +1137,158 @@ __device__ __forceinline__ Tile gemm_tile(const MfmaArgs* args, char* smem, cons
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
       __builtin_amdgcn_wave_barrier();
       __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
+    return next;
+  }
+  if constexpr (kApply<EPI>) {
+    // 16 rows x 128 columns at a time, fp32, as above: X is added before the rounding; its values are fetched two passes ahead.
+    constexpr int kRuns = 8, kPlanes = kTwoPlanes<EPI> ? 2 : 1;
+    typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+    const int piece = lane & 31, col = n0 + wn * 128 + piece * 4;
+    const bool col_ok = col < a.n_out;
+    const size_t matrix = (size_t)tile.slot * a.rows_each * a.n_out;
+    const uint32_t bytes = (uint32_t)a.rows_each * (uint32_t)a.n_out * 2u;
+    const int row_in = row0 - tile.slot * a.rows_each;
+    auto at = [&](int j, int t) {
+      const uint32_t r = (uint32_t)(row_in + wm * 32 * XF + j * 16 + 2 * t + (lane >> 5));
+      return (int)(col_ok ? (r * (uint32_t)a.n_out + (uint32_t)col) * 2u : 0xFFFFFFF0u);
+    };
+    u32x2 old[3][kPlanes][kRuns];
+    auto fetch = [&](int j) {
+#pragma unroll
+      for (int q = 0; q < kPlanes; ++q) {
+        const auto from = __builtin_amdgcn_make_buffer_rsrc((void*)(a.W + q * a.ortho.plane_w + matrix), 0, (int)bytes, 0x00020000);
+#pragma unroll
+        for (int t = 0; t < kRuns; ++t) old[j % 3][q][t] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(from, at(j, t), 0, 0));
+      }
+    };
+    fetch(0);
+    if constexpr (NA > 1) fetch(1);
+#pragma unroll
+    for (int j = 0; j < NA; ++j) {
+      begin_pass(j);
+      if (j + 2 < NA) fetch(j + 2);
+      hold(j);
+      const int r = lane & 15;
+#pragma unroll
+      for (int c = 0; c < NW; ++c) {
+        *(f32x4*)(patch + r * 512 + (((4 * c + quad) ^ r) << 4)) = acc[c][j];
+        feed(j, c, NW);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      u32x2 lo[kRuns];
+#pragma unroll
+      for (int t = 0; t < kRuns; ++t) {
+        const int pr = 2 * t + (lane >> 5);
+        f32x4 v = *(const f32x4*)(patch + pr * 512 + ((piece ^ pr) << 4));
+        const f16x2 x0 = unpack_f16x2(old[j % 3][0][t].x), x1 = unpack_f16x2(old[j % 3][0][t].y);
+        f32x4 x = {(float)x0.x, (float)x0.y, (float)x1.x, (float)x1.y};
+        if constexpr (kPlanes == 2) {
+          const f16x2 y0 = unpack_f16x2(old[j % 3][kPlanes - 1][t].x), y1 = unpack_f16x2(old[j % 3][kPlanes - 1][t].y);
+          x += f32x4{(float)y0.x, (float)y0.y, (float)y1.x, (float)y1.y};
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = fmaf(a.ortho.rho, x[e], v[e] * a.ortho.factor);
+        const u32x2 hi = {pack_f16x2(v[0], v[1]), pack_f16x2(v[2], v[3])};
+        const auto to = __builtin_amdgcn_make_buffer_rsrc((void*)(a.C + matrix), 0, (int)bytes, 0x00020000);
+        __builtin_amdgcn_raw_buffer_store_b64(hi, to, at(j, t), 0, 0);
+        if constexpr (kPlanes == 2) {
+          const f16x2 h0 = unpack_f16x2(hi.x), h1 = unpack_f16x2(hi.y);
+          lo[t] = u32x2{pack_f16x2(v[0] - (float)h0.x, v[1] - (float)h0.y), pack_f16x2(v[2] - (float)h1.x, v[3] - (float)h1.y)};
+          const auto to_lo = __builtin_amdgcn_make_buffer_rsrc((void*)(a.C + a.ortho.plane_c + matrix), 0, (int)bytes, 0x00020000);
+          __builtin_amdgcn_raw_buffer_store_b64(lo[t], to_lo, at(j, t), 0, 0);
+        }
+      }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
+    return next;
+  }
+  if constexpr (kSymmetric<EPI>) {
+    const int row_in = row0 - tile.slot * a.rows_each, m0 = row_in + wm * 32 * XF;  // in its matrix; rows are whole 64s
+    const bool diagonal = row_in == n0;
+    // The product in fp32, out of the compiler's sight: rounded to fp16 in one step with the multiplication here and in two there,
+    // a number half way between two would have a high part of one neighbour and a low part of the other's.
+    auto product = [&](float sum) {
+      float v = sum * a.ortho.factor;
+      asm("" : "+v"(v));
+      return v;
+    };
+    // The diagonal's sums get what else belongs there.  Block j of the wave's rows meets it in one block of columns of one wave.
+    auto on_diagonal = [&](int i, int j) {
+      const int in = lane & 15, r = m0 + j * 16 + in;
+      const size_t d = (size_t)tile.slot * a.rows_each + r;
+      const bool mine = (in >> 2) == quad;
+      float add = a.ortho.on_diagonal;
+      if constexpr (EPI == EPI_SQUARE) add = fmaf(2.f * a.ortho.residual[d], (float)__builtin_bit_cast(_Float16, a.A[d * a.n_out + r]), add);
+      add = mine ? add : 0.f;
+      const int at = in & 3;
+      // (whole vectors: an accumulator whose elements are taken under conditions would live in memory)
+      const f32x4 all = acc[i][j] + f32x4{at == 0 ? add : 0.f, at == 1 ? add : 0.f, at == 2 ? add : 0.f, at == 3 ? add : 0.f};
+      acc[i][j] = all;
+      [[maybe_unused]] const float sum = at == 0 ? all[0] : at == 1 ? all[1] : at == 2 ? all[2] : all[3];
+      if constexpr (EPI == EPI_GRAM) {
+        const float whole = product(sum);
+        if (mine) a.ortho.residual[d] = whole - (float)(_Float16)whole;
+      }
+    };
+    if (diagonal && wm == 0 && wn == 0) {
+#pragma unroll
+      for (int j = 0; j < NA; ++j) on_diagonal(j, j);
+    } else if (diagonal && wm == 1) {
+#pragma unroll
+      for (int j = 0; j < NA; ++j)
+        if (wn == (j + NA) / NW) on_diagonal((j + NA) % NW, j);
+    }
+    // The tile's mirror image: 32 rows become 32 columns, 64 bytes of 128 rows each.  Patch pieces are XORed with the row quad.
+    auto mirror = [&](int p, auto value, uint16_t* dst) {
+      const int jj = p / kPerRows;
+      begin_pass(p);
+      hold(2 * jj);
+      hold(2 * jj + 1);
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int c = 0; c < NW; ++c) {
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const int r = 16 * c + 4 * quad + v, q = 2 * h + ((lane >> 3) & 1);
+            *(_Float16*)(patch + r * 64 + ((q ^ ((r >> 2) & 3)) << 4) + (lane & 7) * 2) = (_Float16)value(c, h, v);
+          }
+          feed(p, h * NW + c, 2 * NW);
+        }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      const auto buf = __builtin_amdgcn_make_buffer_rsrc((void*)(dst + (size_t)tile.slot * a.rows_each * a.n_out), 0,
+                                                         (int)((uint32_t)a.rows_each * (uint32_t)a.n_out * 2u), 0x00020000);
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const int r = t * 16 + (lane >> 2), q = lane & 3;
+        const u32x4_t v = *(const u32x4_t*)(patch + r * 64 + ((q ^ ((r >> 2) & 3)) << 4));
+        const uint32_t row = n0 + wn * 128 + r, at = (row * (uint32_t)a.n_out + (uint32_t)(m0 + 32 * jj + q * 8)) * 2u;
+        __builtin_amdgcn_raw_buffer_store_b128(v, buf, (int)(diagonal || row >= (uint32_t)a.n_out ? 0xFFFFFFF0u : at), 0, 0);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    };
+#pragma unroll
+    for (int jj = 0; jj < XF; ++jj) {
+      auto hi = [&](int c, int h, int v) { return product(acc[c][2 * jj + h][v]); };
+      auto lo = [&](int c, int h, int v) { const float w = product(acc[c][2 * jj + h][v]); return w - (float)(_Float16)w; };
+      if constexpr (kTwoPlanes<EPI>) {
+        pass(4 * jj, hi, a.C, a.n_out, out0, a.n_out);
+        pass(4 * jj + 1, lo, a.C + a.ortho.plane_c, a.n_out, out0, a.n_out);
+        mirror(4 * jj + 2, hi, a.C);
+        mirror(4 * jj + 3, lo, a.C + a.ortho.plane_c);
+      } else {
+        pass(2 * jj, hi, a.C, a.n_out, out0, a.n_out);
+        mirror(2 * jj + 1, hi, a.C);
+      }
     }
     return next;
   }

@@ -220,8 +220,45 @@ __global__ __launch_bounds__(256, 2) void ortho_narrow_kernel(OrthoArgs a) {
 #endif
 }
 
+// Wide tiles where they are many (as use_narrow): the kernel of gemm_mfma.h.  It takes squares without a linear term, and K loops of
+// two steps or more.
 template <int KIND, int PLANES>
-int32_t launch_ortho_narrow(const OrthoArgs& a, hipStream_t st) {
+bool use_wide(const OrthoArgs& a) {
+  const long long m = ceil_div(a.sp, BM), tiles = (KIND == KIND_APPLY ? m * ceil_div(a.lp, BN) : m * (m + 1) / 2) * a.n;
+  return tiles >= 96 && a.sp > BK && (KIND != KIND_SQUARE || (a.lin == 0.f && a.c2 != 0.f));
+}
+template <int KIND, int PLANES>
+int32_t launch_ortho_wide(const OrthoArgs& a, hipStream_t st) {
+  constexpr bool kTwo = PLANES == 2;
+  const size_t small = (size_t)a.n * a.sp * a.sp, large = (size_t)a.n * a.sp * a.lp;
+  MfmaArgs g{};
+  g.matrices = a.n;
+  g.rows_each = a.sp;
+  g.P = (long long)a.n * a.sp;
+  g.ortho.residual = a.residual;
+  if constexpr (KIND == KIND_APPLY) {
+    g.A = a.P, g.W = a.X, g.C = a.out;
+    g.K = a.sp;
+    g.n_out = g.ldw = a.lp;
+    g.ortho = OrthoProduct{small, large, large, 1.f / kOrthoScale, 0.f, a.residual, a.rho};
+  } else {
+    g.A = g.W = KIND == KIND_GRAM ? a.X : a.H;
+    g.C = KIND == KIND_GRAM ? a.H : a.P;
+    g.K = KIND == KIND_GRAM ? a.lp : a.sp;
+    g.w_rows = g.n_out = a.sp;
+    const size_t from = KIND == KIND_GRAM ? large : small;
+    if constexpr (KIND == KIND_GRAM) g.ortho = OrthoProduct{from, from, small, 1.f / kOrthoScale, -a.mu * kOrthoScale * kOrthoScale, a.residual, 0.f};
+    else g.ortho = OrthoProduct{from, from, small, a.c2 / kOrthoScale, a.diag / a.c2 * kOrthoScale * kOrthoScale, a.residual, 0.f};
+  }
+  g.n_tiles = ceil_div(g.n_out, BN);
+  constexpr int kEpi = KIND == KIND_GRAM ? (kTwo ? EPI_GRAM_TWO : EPI_GRAM)
+                       : KIND == KIND_SQUARE ? (kTwo ? EPI_SQUARE_TWO : EPI_SQUARE) : (kTwo ? EPI_APPLY_TWO : EPI_APPLY);
+  return launch_mfma_kernel<kEpi, KIND == KIND_APPLY ? MODE_NN : MODE_NT, false, false, false>(MfmaLaunch<false>{{g}}, st);
+}
+
+template <int KIND, int PLANES>
+int32_t launch_ortho(const OrthoArgs& a, hipStream_t st) {
+  if (use_wide<KIND, PLANES>(a)) return launch_ortho_wide<KIND, PLANES>(a, st);
   const int m = a.sp / kNarrow;
   const long long tiles = KIND == KIND_APPLY ? (long long)m * (a.lp / kNarrow) : (long long)m * (m + 1) / 2;
   hipLaunchKernelGGL((ortho_narrow_kernel<KIND, PLANES>), dim3((unsigned)tiles, (unsigned)a.n), dim3(256), kNarrowLds, st, a);

@@ -237,9 +237,9 @@ int32_t run(const Source& source, const float* old, const lz_orthogonal_shape* s
   for (int k = 0; k < n_steps && rc == LZ_OK; ++k, cur ^= 1) {
     const Step& s = steps[k];
     const OrthoArgs a{w.X[cur], w.H, w.P, w.X[cur ^ 1], w.residual, z.n, z.sp, z.lp, s.mu, s.c2, s.lin, s.diag, s.rho};
-    rc = launch_ortho_narrow<KIND_GRAM, PLANES>(a, st);
-    if (rc == LZ_OK) rc = launch_ortho_narrow<KIND_SQUARE, PLANES>(a, st);
-    if (rc == LZ_OK) rc = launch_ortho_narrow<KIND_APPLY, PLANES>(a, st);
+    rc = launch_ortho<KIND_GRAM, PLANES>(a, st);
+    if (rc == LZ_OK) rc = launch_ortho<KIND_SQUARE, PLANES>(a, st);
+    if (rc == LZ_OK) rc = launch_ortho<KIND_APPLY, PLANES>(a, st);
   }
   if (rc != LZ_OK) return rc;
   hipLaunchKernelGGL((finish_kernel<Elem, UPDATE, PLANES>), dim3(tiles, z.n), dim3(256), 0, st, w.X[cur], z, (Elem*)out, update);

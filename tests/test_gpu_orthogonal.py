@@ -88,6 +88,16 @@ def test_orthogonalize(size, dtype, kind):
     assert (d <= bound).all(), (d / bound).max()
 
 
+# as many tiles as the wide kernel takes, whole ones and of 64, 128 and 192 rows; several bands of them
+WIDE = [(40, 300, 500), (36, 330, 440), (34, 380, 400), (7, 1090, 1150), (11, 1300, 770)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("size", WIDE, ids=lambda s: "x".join(map(str, s)))
+def test_many_tiles(size, dtype):
+    test_orthogonalize(size, dtype, "noise")
+
+
 @pytest.mark.parametrize("coef", [CUBIC, ((2.0, -1.5, 0.5),) * 3, ((1.0, 0.0, 0.0),), ((0.0, 0.0, 1.0),), ((1.0, -2.0, 0.25),),
                                   ((3.4445, -4.7750, 2.0315),) * 3 + ((1.875, -1.25, 0.375),) * 2], ids=str)
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
