@@ -30,6 +30,7 @@ struct OrthoArgs {
   float* residual;    // [n][sp]: what rounding took from H's diagonal (one plane)
   int n, sp, lp;
   float mu, c2, lin, diag, rho;  // diag = q0 - rho
+  int pairs;                     // of planes that a product of two planes sums: 3, or 1: hi hi alone
 };
 
 __device__ __forceinline__ float f16_value(uint16_t b) { return (float)__builtin_bit_cast(_Float16, b); }
@@ -99,7 +100,7 @@ __global__ __launch_bounds__(256, 2) void ortho_narrow_kernel(OrthoArgs a) {
     if constexpr (TB) voffW[i] = (int)(((uint32_t)r * (uint32_t)ldw + (uint32_t)(n0 + ((lane & 7) ^ swz_narrow(r)) * 8)) * 2u);
     else voffW[i] = (int)(((uint32_t)(n0 + r) * (uint32_t)K + (uint32_t)chunk * 8u) * 2u);
   }
-  const int k_steps = K / BK, all_steps = PLANES == 2 ? 3 * k_steps : k_steps;
+  const int k_steps = K / BK, all_steps = PLANES == 2 ? a.pairs * k_steps : k_steps;
   int seg = 0, k = 0;  // of the next step to load: which pair of planes, step within it
   auto issue = [&](bool real, int stage) {  // a step past the end writes zeros, without memory traffic
     const i32x4 wa = rsrc_words(matA + (seg == 2 ? planeA : 0), real ? extentA : 0), ww = rsrc_words(matW + (seg == 1 ? planeW : 0), real ? extentW : 0);
@@ -235,20 +236,19 @@ int32_t launch_ortho_wide(const OrthoArgs& a, hipStream_t st) {
   g.matrices = a.n;
   g.rows_each = a.sp;
   g.P = (long long)a.n * a.sp;
-  g.ortho.residual = a.residual;
   if constexpr (KIND == KIND_APPLY) {
     g.A = a.P, g.W = a.X, g.C = a.out;
     g.K = a.sp;
     g.n_out = g.ldw = a.lp;
-    g.ortho = OrthoProduct{small, large, large, 1.f / kOrthoScale, 0.f, a.residual, a.rho};
+    g.ortho = OrthoProduct{small, large, large, 1.f / kOrthoScale, 0.f, a.residual, a.rho, a.pairs};
   } else {
     g.A = g.W = KIND == KIND_GRAM ? a.X : a.H;
     g.C = KIND == KIND_GRAM ? a.H : a.P;
     g.K = KIND == KIND_GRAM ? a.lp : a.sp;
     g.w_rows = g.n_out = a.sp;
     const size_t from = KIND == KIND_GRAM ? large : small;
-    if constexpr (KIND == KIND_GRAM) g.ortho = OrthoProduct{from, from, small, 1.f / kOrthoScale, -a.mu * kOrthoScale * kOrthoScale, a.residual, 0.f};
-    else g.ortho = OrthoProduct{from, from, small, a.c2 / kOrthoScale, a.diag / a.c2 * kOrthoScale * kOrthoScale, a.residual, 0.f};
+    if constexpr (KIND == KIND_GRAM) g.ortho = OrthoProduct{from, from, small, 1.f / kOrthoScale, -a.mu * kOrthoScale * kOrthoScale, a.residual, 0.f, a.pairs};
+    else g.ortho = OrthoProduct{from, from, small, a.c2 / kOrthoScale, a.diag / a.c2 * kOrthoScale * kOrthoScale, a.residual, 0.f, a.pairs};
   }
   g.n_tiles = ceil_div(g.n_out, BN);
   constexpr int kEpi = KIND == KIND_GRAM ? (kTwo ? EPI_GRAM_TWO : EPI_GRAM)

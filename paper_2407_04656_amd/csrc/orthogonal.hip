@@ -185,11 +185,18 @@ __global__ __launch_bounds__(256) void finish_kernel(const uint16_t* __restrict_
 // The steps' constants.
 struct Step {
   float mu, c2, lin, diag, rho;
+  bool coarse;  // with products of one plane where X has two
 };
 
 // false: coefficients that can lead past kMostNorm.  Singular values start in [0, 1]; a step takes x to x q(x^2).
-bool plan_steps(const float* coef, int steps, int planes, Step* out) {
-  double most = 1.0;
+//
+// coarse: X <- rho X + P X with rho = c0 is off by the rounding of one plane times P / c0, and most directions' P is about c1 s, s their
+// singular value squared: 1 / small at first (a flat spectrum), c0^2 times as much after a step.  Up to 0.02 (the first two of the
+// usual five steps from a small side of 823 on, the first from 70 on) a step's products take one plane, a third of the work.  Off by then,
+// 2-norm: 5e-6 to 1.3e-5 at 128 x 256 (flat to e^-10 falling spectra), 7e-6 to 2e-5 at 1408 x 2048; in two planes 1e-6, with the third
+// step in one too 1.3e-4 to 3e-4.  A weight of size 0.02 that moves by 2e-3 / sqrt(small) is off by less than 1e-7 of it.
+bool plan_steps(const float* coef, int steps, int planes, int small, Step* out) {
+  double most = 1.0, typical = small > 0 ? 1.0 / small : 0.0;
   for (int k = 0; k < steps; ++k) {
     const double a = coef[3 * k], b = coef[3 * k + 1], c = coef[3 * k + 2];
     if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
@@ -198,7 +205,9 @@ bool plan_steps(const float* coef, int steps, int planes, Step* out) {
     if (!(std::fabs(mu) <= 2.0)) mu = 0.0;  // far off [0, 1]: H would be mu and little else
     // rho X + P X: P is small, and its rounding with it, where q is near rho, which the last steps take near 1; not above c0, which q
     // is for small singular values.  One plane: the first steps enlarge those, and an 11-bit diagonal of P would be what is off most.
-    const double rho = planes == 1 && 2 * k < steps - 1 ? a : std::fmin(a, 1.0);
+    const bool coarse = small > 0 && a > 0.0 && (std::fabs(b) + std::fabs(c) * typical) * typical <= 0.02 * a;
+    typical *= a * a;
+    const double rho = coarse || (planes == 1 && 2 * k < steps - 1) ? a : std::fmin(a, 1.0);
     const double q0 = a + b * mu + c * mu * mu;
     auto q = [&](double s) { return a + b * s + c * s * s; };
     double p = std::fmax(std::fabs(q(0) - rho), std::fabs(q(top) - rho));
@@ -218,7 +227,7 @@ bool plan_steps(const float* coef, int steps, int planes, Step* out) {
     }
     const double h = std::fmax(std::fabs(mu), std::fabs(top - mu));
     if (!(h <= kMostNorm && p <= kMostNorm && next <= kMostNorm)) return false;
-    out[k] = Step{(float)mu, (float)c, mu != 0.0 ? 0.f : (float)b, (float)(q0 - rho), (float)rho};
+    out[k] = Step{(float)mu, (float)c, mu != 0.0 ? 0.f : (float)b, (float)(q0 - rho), (float)rho, coarse};
     most = next;
   }
   return true;
@@ -236,9 +245,9 @@ int32_t run(const Source& source, const float* old, const lz_orthogonal_shape* s
   int cur = 0;
   for (int k = 0; k < n_steps && rc == LZ_OK; ++k, cur ^= 1) {
     const Step& s = steps[k];
-    const OrthoArgs a{w.X[cur], w.H, w.P, w.X[cur ^ 1], w.residual, z.n, z.sp, z.lp, s.mu, s.c2, s.lin, s.diag, s.rho};
-    rc = launch_ortho<KIND_GRAM, PLANES>(a, st);
-    if (rc == LZ_OK) rc = launch_ortho<KIND_SQUARE, PLANES>(a, st);
+    const OrthoArgs a{w.X[cur], w.H, w.P, w.X[cur ^ 1], w.residual, z.n, z.sp, z.lp, s.mu, s.c2, s.lin, s.diag, s.rho, s.coarse ? 1 : 3};
+    rc = s.coarse ? launch_ortho<KIND_GRAM, 1>(a, st) : launch_ortho<KIND_GRAM, PLANES>(a, st);
+    if (rc == LZ_OK) rc = s.coarse ? launch_ortho<KIND_SQUARE, 1>(a, st) : launch_ortho<KIND_SQUARE, PLANES>(a, st);
     if (rc == LZ_OK) rc = launch_ortho<KIND_APPLY, PLANES>(a, st);
   }
   if (rc != LZ_OK) return rc;
@@ -246,10 +255,10 @@ int32_t run(const Source& source, const float* old, const lz_orthogonal_shape* s
   return lz::launch_status();
 }
 
-int32_t check(const lz_orthogonal_shape* s, const float* coef, int32_t steps, float eps, int planes, void* ws, size_t ws_bytes, OrthoWorkspace* w,
+int32_t check(const lz_orthogonal_shape* s, const float* coef, int32_t steps, float eps, int planes, bool update, void* ws, size_t ws_bytes, OrthoWorkspace* w,
               Step* plan) {
   if (!shape_ok(s)) return LZ_ESHAPE;
-  if (!coef || steps < 1 || steps > kMostSteps || !(eps >= 0.f) || !std::isfinite(eps) || !plan_steps(coef, steps, planes, plan)) return LZ_EINVAL;
+  if (!coef || steps < 1 || steps > kMostSteps || !(eps >= 0.f) || !std::isfinite(eps) || !plan_steps(coef, steps, planes, update ? (s->rows < s->cols ? s->rows : s->cols) : 0, plan)) return LZ_EINVAL;
   *w = carve(ws, s);
   if (!ws || (uintptr_t)ws % 256 != 0 || ws_bytes < w->bytes) return LZ_EWORKSPACE;
   return LZ_OK;
@@ -265,7 +274,7 @@ extern "C" int32_t lz_orthogonalize(const void* g, const lz_orthogonal_shape* sh
                                     void* ws, size_t ws_bytes, void* stream) {
   OrthoWorkspace w;
   Step plan[kMostSteps];
-  const int32_t rc = check(shape, coef, steps, eps, shape && shape->dtype == LZ_F32 ? 2 : 1, ws, ws_bytes, &w, plan);
+  const int32_t rc = check(shape, coef, steps, eps, shape && shape->dtype == LZ_F32 ? 2 : 1, false, ws, ws_bytes, &w, plan);
   if (rc != LZ_OK) return rc;
   if (!g || !out) return LZ_EINVAL;
   const Source source{g, nullptr, 0.f, 0};
@@ -280,7 +289,7 @@ extern "C" int32_t lz_orthogonal_step(const void* g, const float* momentum, cons
   if (!options) return LZ_EINVAL;
   OrthoWorkspace w;
   Step plan[kMostSteps];
-  const int32_t rc = check(shape, options->coef, options->steps, options->eps, 2, ws, ws_bytes, &w, plan);
+  const int32_t rc = check(shape, options->coef, options->steps, options->eps, 2, true, ws, ws_bytes, &w, plan);
   if (rc != LZ_OK) return rc;
   if (!g || !momentum || !master || !momentum_out || !master_out || slots < 0 || (slots > 0 && (!slot_expert || !slot_weights))) return LZ_EINVAL;
   const Source source{g, momentum_out, (float)options->mu, options->nesterov};
