@@ -1,21 +1,12 @@
 // Orthogonalised updates: Newton-Schulz steps of stacks of matrices, and the optimizer step around them.
 #include <cmath>
 
-#include "gemm_orthogonal.h"
-#include "gemm_f32.h"
+#include "orthogonal_thin.h"
 
 namespace {
 
 constexpr int kMostSteps = 16;
 constexpr double kMostNorm = 3.9;  // of what is kept in fp16: 3.9 * 2^14 < 65504
-constexpr int kNormBlocks = 64;    // partial sums of a matrix
-
-inline int up64(int v) { return (v + 63) / 64 * 64; }
-
-struct OrthoSize {
-  int n, rows, cols, sp, lp;
-  bool tall;  // rows > cols: X is the transpose
-};
 inline OrthoSize size_of(const lz_orthogonal_shape* s) {
   const bool tall = s->rows > s->cols;
   return OrthoSize{s->n, s->rows, s->cols, up64(tall ? s->cols : s->rows), up64(tall ? s->rows : s->cols), tall};
@@ -27,10 +18,13 @@ inline bool shape_ok(const lz_orthogonal_shape* s) {
   return (long long)z.sp * z.lp < (1ll << 30);
 }
 
+inline int small_side(const lz_orthogonal_shape* s) { return s->rows < s->cols ? s->rows : s->cols; }
+
 struct OrthoWorkspace {
-  double* sums;     // [n, kNormBlocks]
+  double* sums;     // [n, norm_blocks()]
   float* residual;  // [n, sp]
-  uint16_t *X[2], *H, *P;  // two planes each
+  uint16_t *X[2], *H, *P;  // two planes each; thin matrices: X column by column
+  float* part[2];          // thin matrices: parts of G
   size_t bytes;
 };
 OrthoWorkspace carve(void* ws, const lz_orthogonal_shape* s) {
@@ -42,8 +36,15 @@ OrthoWorkspace carve(void* ws, const lz_orthogonal_shape* s) {
     p += lz::align256(bytes);
     return r;
   };
-  w.sums = (double*)take(sizeof(double) * z.n * kNormBlocks);
+  w.sums = (double*)take(sizeof(double) * z.n * norm_blocks((size_t)z.rows * z.cols));
   w.residual = (float*)take(sizeof(float) * z.n * z.sp);
+  if (small_side(s) <= kThinMost) {
+    const int sp = thin_side(small_side(s));
+    for (auto& x : w.X) x = (uint16_t*)take(4 * (size_t)z.n * sp * z.lp);
+    for (auto& g : w.part) g = (float*)take(4 * (size_t)z.n * thin_parts(z.n, z.lp) * sp * sp);
+    w.bytes = size_t(p - (char*)ws);
+    return w;
+  }
   for (auto& x : w.X) x = (uint16_t*)take(4 * (size_t)z.n * z.sp * z.lp);
   w.H = (uint16_t*)take(4 * (size_t)z.n * z.sp * z.sp);
   w.P = (uint16_t*)take(4 * (size_t)z.n * z.sp * z.sp);
@@ -51,54 +52,70 @@ OrthoWorkspace carve(void* ws, const lz_orthogonal_shape* s) {
   return w;
 }
 
-// What is orthogonalised: the gradient, or the gradient and its momentum.
-struct Source {
-  const void* g;
-  const float* momentum;  // the new one, where there is one
-  float mu;
-  int nesterov;
-};
+// Sums of squares in 64 bits (fp32 inputs of any size), several of every matrix; UPDATE: the new momentum on the way.  `whole`: matrices
+// of whole aligned pieces of 8.
 template <typename Elem, bool UPDATE>
-__device__ __forceinline__ float source_value(const Source& s, size_t i) {
-  if constexpr (!UPDATE) return load_elem<Elem>((const Elem*)s.g + i);
-  else return s.nesterov ? fmaf(s.mu, s.momentum[i], load_elem<Elem>((const Elem*)s.g + i)) : s.momentum[i];
-}
-
-// Sums of squares in 64 bits (fp32 inputs of any size), kNormBlocks of every matrix; UPDATE: the new momentum on the way.
-template <typename Elem, bool UPDATE>
-__global__ __launch_bounds__(256) void norm_kernel(Source s, const float* old, float* momentum, size_t elems,
+__global__ __launch_bounds__(256) void norm_kernel(Source s, const float* old, float* momentum, size_t elems, bool whole,
                                                    double* __restrict__ sums) {
   __shared__ double waves[4];
-  const size_t base = blockIdx.y * elems;
+  const size_t base = blockIdx.y * elems, stride = (size_t)gridDim.x * 256, first = (size_t)blockIdx.x * 256 + threadIdx.x;
+  const Elem* const grad = (const Elem*)s.g + base;
   double sum = 0.0;
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < elems; i += kNormBlocks * 256) {
-    float u;
-    if constexpr (UPDATE) {
-      const float g = load_elem<Elem>((const Elem*)s.g + base + i), m = fmaf(s.mu, old[base + i], g);
-      momentum[base + i] = m;
-      u = s.nesterov ? fmaf(s.mu, m, g) : m;
-    } else {
-      u = load_elem<Elem>((const Elem*)s.g + base + i);
+  auto next = [&](float g, float was, float& m) {  // what is orthogonalised
+    if constexpr (!UPDATE) return g;
+    m = fmaf(s.mu, was, g);
+    return s.nesterov ? fmaf(s.mu, m, g) : m;
+  };
+  if (whole) {
+    for (size_t p = first; p < elems / 8; p += stride) {
+      float g[8], was[8] = {}, m[8];
+      if constexpr (sizeof(Elem) == 4) {
+        *(f32x4*)g = *(const f32x4*)(grad + p * 8);
+        *(f32x4*)(g + 4) = *(const f32x4*)(grad + p * 8 + 4);
+      } else {
+        const u32x4_t v = *(const u32x4_t*)(grad + p * 8);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          g[2 * e] = __uint_as_float(v[e] << 16);
+          g[2 * e + 1] = __uint_as_float(v[e] & 0xFFFF0000u);
+        }
+      }
+      if constexpr (UPDATE) {
+        *(f32x4*)was = *(const f32x4*)(old + base + p * 8);
+        *(f32x4*)(was + 4) = *(const f32x4*)(old + base + p * 8 + 4);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const double u = next(g[e], was[e], m[e]);
+        sum = fma(u, u, sum);
+      }
+      if constexpr (UPDATE) {
+        *(f32x4*)(momentum + base + p * 8) = *(f32x4*)m;
+        *(f32x4*)(momentum + base + p * 8 + 4) = *(f32x4*)(m + 4);
+      }
     }
-    sum = fma((double)u, (double)u, sum);
+  } else {
+    for (size_t i = first; i < elems; i += stride) {
+      float was = 0.f, m;
+      if constexpr (UPDATE) was = old[base + i];
+      const double u = next(load_elem<Elem>(grad + i), was, m);
+      if constexpr (UPDATE) momentum[base + i] = m;
+      sum = fma(u, u, sum);
+    }
   }
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
   if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = sum;
   __syncthreads();
-  if (threadIdx.x == 0) sums[(size_t)blockIdx.y * kNormBlocks + blockIdx.x] = waves[0] + waves[1] + waves[2] + waves[3];
+  if (threadIdx.x == 0) sums[(size_t)blockIdx.y * gridDim.x + blockIdx.x] = waves[0] + waves[1] + waves[2] + waves[3];
 }
 
 // 64 x 64 of a matrix as it lies -> X, transposed where it is tall, scaled to norm 1 (times 2^14), zeros around it.
 template <typename Elem, bool UPDATE, int PLANES>
-__global__ __launch_bounds__(256) void load_kernel(Source s, OrthoSize z, const double* __restrict__ sums, float eps, uint16_t* __restrict__ X) {
+__global__ __launch_bounds__(256) void load_kernel(Source s, OrthoSize z, const double* __restrict__ sums, int blocks, float eps, uint16_t* __restrict__ X) {
   __shared__ float tile[64][65];
   const int lane = threadIdx.x & 63;
-  double total = sums[(size_t)blockIdx.y * kNormBlocks + lane];
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) total += __shfl_xor(total, off, 64);
-  const double norm = sqrt(total) + (double)eps;
-  const float inv = (float)(1.0 / norm);
+  const float inv = inverse_norm(sums + (size_t)blockIdx.y * blocks, blocks, eps);
   const int tiles_c = (z.tall ? z.sp : z.lp) / 64, r0 = blockIdx.x / tiles_c * 64, c0 = blockIdx.x % tiles_c * 64;
   const size_t base = (size_t)blockIdx.y * z.rows * z.cols;
   for (int i = 0; i < 16; ++i) {
@@ -120,15 +137,6 @@ __global__ __launch_bounds__(256) void load_kernel(Source s, OrthoSize z, const 
     store_planes8<PLANES>(to + (size_t)row * z.lp + col, plane, v);
   }
 }
-
-struct Update {
-  float keep, rate;  // 1 - lr weight_decay, lr scale
-  const float* master;
-  float* master_out;
-  const int32_t* slot_expert;
-  int slots;
-  void* slot_weights;
-};
 
 // X -> the result as it lies; UPDATE: the weights, and their copies in the slots.
 template <typename Elem, bool UPDATE, int PLANES>
@@ -184,7 +192,7 @@ __global__ __launch_bounds__(256) void finish_kernel(const uint16_t* __restrict_
 
 // The steps' constants.
 struct Step {
-  float mu, c2, lin, diag, rho;
+  float mu, c2, lin, diag, rho, q0;
   bool coarse;  // with products of one plane where X has two
 };
 
@@ -195,18 +203,23 @@ struct Step {
 // usual five steps from a small side of 823 on, the first from 70 on) a step's products take one plane, a third of the work.  Off by then,
 // 2-norm: 5e-6 to 1.3e-5 at 128 x 256 (flat to e^-10 falling spectra), 7e-6 to 2e-5 at 1408 x 2048; in two planes 1e-6, with the third
 // step in one too 1.3e-4 to 3e-4.  A weight of size 0.02 that moves by 2e-3 / sqrt(small) is off by less than 1e-7 of it.
-bool plan_steps(const float* coef, int steps, int planes, int small, Step* out) {
-  double most = 1.0, typical = small > 0 ? 1.0 / small : 0.0;
+//
+// Thin matrices have no square to save: while most directions are small, H = G holds what they are off 0 by with all its bits, where
+// G - mu would be mu and little else (70 x 33 x 40 of a few large directions, two planes: 6e-6 of the result with mu throughout).
+bool plan_steps(const float* coef, int steps, int planes, int small, bool update, Step* out) {
+  const bool thin = small <= kThinMost;
+  double most = 1.0, typical = 1.0 / small;
   for (int k = 0; k < steps; ++k) {
     const double a = coef[3 * k], b = coef[3 * k + 1], c = coef[3 * k + 2];
     if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
     const double top = most * most;
     double mu = c != 0.0 ? -b / (2 * c) : 0.0;
-    if (!(std::fabs(mu) <= 2.0)) mu = 0.0;  // far off [0, 1]: H would be mu and little else
+    const double p_typical = (std::fabs(b) + std::fabs(c) * typical) * typical;
+    const bool coarse = update && !thin && a > 0.0 && p_typical <= 0.02 * a;
+    if (!(std::fabs(mu) <= 2.0) || (thin && p_typical <= 0.3 * std::fabs(a))) mu = 0.0;  // (far off [0, 1] H would be mu and little else)
+    typical *= a * a;
     // rho X + P X: P is small, and its rounding with it, where q is near rho, which the last steps take near 1; not above c0, which q
     // is for small singular values.  One plane: the first steps enlarge those, and an 11-bit diagonal of P would be what is off most.
-    const bool coarse = small > 0 && a > 0.0 && (std::fabs(b) + std::fabs(c) * typical) * typical <= 0.02 * a;
-    typical *= a * a;
     const double rho = coarse || (planes == 1 && 2 * k < steps - 1) ? a : std::fmin(a, 1.0);
     const double q0 = a + b * mu + c * mu * mu;
     auto q = [&](double s) { return a + b * s + c * s * s; };
@@ -227,10 +240,25 @@ bool plan_steps(const float* coef, int steps, int planes, int small, Step* out) 
     }
     const double h = std::fmax(std::fabs(mu), std::fabs(top - mu));
     if (!(h <= kMostNorm && p <= kMostNorm && next <= kMostNorm)) return false;
-    out[k] = Step{(float)mu, (float)c, mu != 0.0 ? 0.f : (float)b, (float)(q0 - rho), (float)rho, coarse};
+    out[k] = Step{(float)mu, (float)c, mu != 0.0 ? 0.f : (float)b, (float)(q0 - rho), (float)rho, (float)q0, coarse};
     most = next;
   }
   return true;
+}
+
+template <typename Elem, bool UPDATE, int PLANES, int SP>
+int32_t run_thin(const Source& source, const OrthoSize& z, const Step* steps, int n_steps, float eps, void* out, const Update& update,
+                 const OrthoWorkspace& w, hipStream_t st) {
+  ThinArgs a{w.sums, norm_blocks((size_t)z.rows * z.cols), eps, nullptr, w.X[0], nullptr, w.part[0], thin_parts(z.n, z.lp), z.lp, 0.f, 0.f, 0.f, 0.f};
+  int32_t rc = launch_thin<Elem, UPDATE, THIN_FIRST, SP, PLANES>(a, source, z, out, update, st);
+  for (int k = 0; k < n_steps && rc == LZ_OK; ++k) {
+    const Step& s = steps[k];
+    a.from = w.X[k & 1], a.to = w.X[(k + 1) & 1], a.part_in = w.part[k & 1], a.part_out = w.part[(k + 1) & 1];
+    a.mu = s.mu, a.c2 = s.c2, a.lin = s.lin, a.q0 = s.q0;
+    rc = k + 1 < n_steps ? launch_thin<Elem, UPDATE, THIN_STEP, SP, PLANES>(a, source, z, out, update, st)
+                         : launch_thin<Elem, UPDATE, THIN_LAST, SP, PLANES>(a, source, z, out, update, st);
+  }
+  return rc;
 }
 
 template <typename Elem, bool UPDATE, int PLANES>
@@ -239,8 +267,18 @@ int32_t run(const Source& source, const float* old, const lz_orthogonal_shape* s
   const OrthoSize z = size_of(shape);
   const unsigned tiles = (unsigned)((size_t)z.sp * z.lp / 4096);
   const size_t elems = (size_t)z.rows * z.cols;
-  hipLaunchKernelGGL((norm_kernel<Elem, UPDATE>), dim3(kNormBlocks, z.n), dim3(256), 0, st, source, old, (float*)source.momentum, elems, w.sums);
-  hipLaunchKernelGGL((load_kernel<Elem, UPDATE, PLANES>), dim3(tiles, z.n), dim3(256), 0, st, source, z, w.sums, eps, w.X[0]);
+  const int norms = norm_blocks(elems);
+  const bool whole = elems % 8 == 0 && aligned16(source.g) && aligned16(old) && aligned16(source.momentum);
+  hipLaunchKernelGGL((norm_kernel<Elem, UPDATE>), dim3(norms, z.n), dim3(256), 0, st, source, old, (float*)source.momentum, elems, whole, w.sums);
+  if (const int small = small_side(shape); small <= kThinMost) {
+    const int32_t rc = lz::launch_status();
+    if (rc != LZ_OK) return rc;
+    const int sp = thin_side(small);
+    return sp == 32   ? run_thin<Elem, UPDATE, PLANES, 32>(source, z, steps, n_steps, eps, out, update, w, st)
+           : sp == 64 ? run_thin<Elem, UPDATE, PLANES, 64>(source, z, steps, n_steps, eps, out, update, w, st)
+                      : run_thin<Elem, UPDATE, PLANES, 128>(source, z, steps, n_steps, eps, out, update, w, st);
+  }
+  hipLaunchKernelGGL((load_kernel<Elem, UPDATE, PLANES>), dim3(tiles, z.n), dim3(256), 0, st, source, z, w.sums, norms, eps, w.X[0]);
   int32_t rc = lz::launch_status();
   int cur = 0;
   for (int k = 0; k < n_steps && rc == LZ_OK; ++k, cur ^= 1) {
@@ -258,7 +296,7 @@ int32_t run(const Source& source, const float* old, const lz_orthogonal_shape* s
 int32_t check(const lz_orthogonal_shape* s, const float* coef, int32_t steps, float eps, int planes, bool update, void* ws, size_t ws_bytes, OrthoWorkspace* w,
               Step* plan) {
   if (!shape_ok(s)) return LZ_ESHAPE;
-  if (!coef || steps < 1 || steps > kMostSteps || !(eps >= 0.f) || !std::isfinite(eps) || !plan_steps(coef, steps, planes, update ? (s->rows < s->cols ? s->rows : s->cols) : 0, plan)) return LZ_EINVAL;
+  if (!coef || steps < 1 || steps > kMostSteps || !(eps >= 0.f) || !std::isfinite(eps) || !plan_steps(coef, steps, planes, small_side(s), update, plan)) return LZ_EINVAL;
   *w = carve(ws, s);
   if (!ws || (uintptr_t)ws % 256 != 0 || ws_bytes < w->bytes) return LZ_EWORKSPACE;
   return LZ_OK;

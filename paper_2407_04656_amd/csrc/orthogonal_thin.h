@@ -1,0 +1,333 @@
+// Orthogonalised updates of matrices whose shorter side is at most 128: a step in one launch.  Device code of orthogonal.hip, not
+// part of the C ABI.
+//
+// G is small here, and every workgroup holds all of H = G - mu I in LDS.  It takes 64 columns of X at a time,
+//
+//   Y = H X,   X' = q0 X + lin Y + c2 H Y,   G' += X' X'^T
+//
+// and leaves its part of G' for the next launch, whose workgroups each add the parts up.  What bounds the products of such matrices in
+// launches of their own (three a step) is the launches: 17 of 5 us for 8 matrices of 128 x 256, where this takes 7.
+// X is kept column by column (k of the products contiguous), fp16 in one plane or two as in gemm_orthogonal.h.  H in one plane gets what
+// rounding took from its diagonal back as r X and r Y.  In two planes the sums of a block of columns are added in fp32 by the
+// vector unit: the matrix unit cuts off what it aligns away, which over thousands of columns adds up (32 x 24 x 1600: 4e-6 of the result).
+#pragma once
+#include "gemm_f32.h"
+#include "gemm_orthogonal.h"
+
+namespace {
+
+// Partial sums of a matrix: workgroups of 8192 elements or more, enough of them for a few large matrices.
+constexpr int kMostNormBlocks = 512;
+inline int norm_blocks(size_t elems) {
+  const size_t b = elems / 8192;
+  return (int)(b < 1 ? 1 : b < kMostNormBlocks ? b : kMostNormBlocks);
+}
+inline int up64(int v) { return (v + 63) / 64 * 64; }
+
+struct OrthoSize {
+  int n, rows, cols, sp, lp;
+  bool tall;  // rows > cols: X is the transpose
+};
+// What is orthogonalised: the gradient, or the gradient and its momentum.
+struct Source {
+  const void* g;
+  const float* momentum;  // the new one, where there is one
+  float mu;
+  int nesterov;
+};
+// 1 / (norm + eps) of a matrix, in every lane
+__device__ __forceinline__ float inverse_norm(const double* __restrict__ sums, int blocks, float eps) {
+  double total = 0.0;
+  for (int i = threadIdx.x & 63; i < blocks; i += 64) total += sums[i];
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) total += __shfl_xor(total, off, 64);
+  return (float)(1.0 / (sqrt(total) + (double)eps));
+}
+template <typename Elem, bool UPDATE>
+__device__ __forceinline__ float source_value(const Source& s, size_t i) {
+  if constexpr (!UPDATE) return load_elem<Elem>((const Elem*)s.g + i);
+  else return s.nesterov ? fmaf(s.mu, s.momentum[i], load_elem<Elem>((const Elem*)s.g + i)) : s.momentum[i];
+}
+
+struct Update {
+  float keep, rate;  // 1 - lr weight_decay, lr scale
+  const float* master;
+  float* master_out;
+  const int32_t* slot_expert;
+  int slots;
+  void* slot_weights;
+};
+
+
+enum { THIN_FIRST = 0, THIN_STEP = 1, THIN_LAST = 2 };
+constexpr int kThinMost = 128;     // shorter side
+constexpr int kThinBlock = 64;     // columns at a time
+constexpr int kThinMostParts = 16; // workgroups of a matrix
+
+struct ThinArgs {
+  const double* sums;     // FIRST: of squares, norm_blocks of a matrix
+  int norm_blocks;
+  float eps;
+  uint16_t *from, *to;    // [planes][n][columns up to 64s][SP]
+  const float* part_in;   // [n][parts][SP][SP]
+  float* part_out;
+  int parts, columns;     // columns: up to whole blocks
+  float mu, c2, lin, q0;
+};
+
+template <int SP, int PLANES>
+struct ThinLds {
+  static constexpr int kPitch = SP * 2 + 16;  // bytes of a row
+  static constexpr int kH = SP * kPitch, kX = kThinBlock * kPitch;  // of a plane
+  static constexpr int kTile = kThinBlock * (SP + 1) * 4;           // the result, fp32
+  static constexpr int x = PLANES * kH, y = x + PLANES * kX, r = x + (2 * PLANES * kX > kTile ? 2 * PLANES * kX : kTile), bytes = r + SP * 4;
+};
+
+// blockIdx.x = part of the columns, blockIdx.y = matrix
+template <typename Elem, bool UPDATE, int MODE, int SP, int PLANES>
+__global__ __launch_bounds__(256) void thin_step_kernel(ThinArgs a, Source source, OrthoSize z, Elem* __restrict__ out, Update u) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  using L = ThinLds<SP, PLANES>;
+  constexpr int kPitch = L::kPitch, NB = SP / 16, KS = SP / 32;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  char* const lds_h = smem;
+  char* const lds_x = smem + L::x;
+  char* const lds_y = smem + L::y;
+  float* const lds_r = (float*)(smem + L::r);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), in = lane & 15, quad = lane >> 4;
+  const int small = z.tall ? z.cols : z.rows, large = z.tall ? z.rows : z.cols;
+  const size_t matrix = blockIdx.y;
+  const size_t plane = (size_t)z.n * a.columns * SP, base = matrix * a.columns * SP;
+  const size_t elems = (size_t)z.rows * z.cols;
+  float inv = 0.f;
+  if constexpr (MODE == THIN_FIRST) {
+    inv = inverse_norm(a.sums + matrix * a.norm_blocks, a.norm_blocks, a.eps);
+  } else {
+    // H from the parts of G (at 2^28 times its size)
+    const float* const part = a.part_in + matrix * a.parts * (SP * SP);
+    for (int i = tid; i < SP * SP / 8; i += 256) {
+      float v[8] = {};
+      for (int p = 0; p < a.parts; ++p) {
+        const f32x4 v0 = *(const f32x4*)(part + (size_t)p * (SP * SP) + i * 8), v1 = *(const f32x4*)(part + (size_t)p * (SP * SP) + i * 8 + 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += v0[e], v[e + 4] += v1[e];
+      }
+      const int row = i / (SP / 8), col = i % (SP / 8) * 8;
+      f16x8 hi, lo;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float h = fmaf(v[e], 1.f / kOrthoScale, row == col + e ? -a.mu * kOrthoScale : 0.f);
+        asm("" : "+v"(h));  // rounded to fp32 before it is to fp16, for both parts
+        hi[e] = (_Float16)h;
+        lo[e] = (_Float16)(h - (float)hi[e]);
+        if (PLANES == 1 && row == col + e) lds_r[row] = (h - (float)hi[e]) * (1.f / kOrthoScale);
+      }
+      *(f16x8*)(lds_h + row * kPitch + col * 2) = hi;
+      if constexpr (PLANES == 2) *(f16x8*)(lds_h + L::kH + row * kPitch + col * 2) = lo;
+    }
+  }
+  f32x4 gram[NB * NB / 4] = {};
+  const int blocks = a.columns / kThinBlock;
+  const int first = (int)((long long)blocks * blockIdx.x / a.parts), last = (int)((long long)blocks * (blockIdx.x + 1) / a.parts);
+  for (int b = first; b < last; ++b) {
+    __syncthreads();  // H is there; nobody reads the last block any more
+    if constexpr (MODE == THIN_FIRST) {
+      for (int i = tid; i < kThinBlock * SP; i += 256) {
+        const int c = z.tall ? i / SP : i % kThinBlock, r = z.tall ? i % SP : i / kThinBlock, col = b * kThinBlock + c;
+        float v = 0.f;
+        if (r < small && col < large)
+          v = source_value<Elem, UPDATE>(source, matrix * elems + (z.tall ? (size_t)col * z.cols + r : (size_t)r * z.cols + col)) * inv * kOrthoScale;
+        asm("" : "+v"(v));
+        const _Float16 hi = (_Float16)v;
+        *(_Float16*)(lds_x + c * kPitch + r * 2) = hi;
+        if constexpr (PLANES == 2) *(_Float16*)(lds_x + L::kX + c * kPitch + r * 2) = (_Float16)(v - (float)hi);
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < PLANES; ++q)
+        for (int i = tid; i < kThinBlock * SP / 8; i += 256)
+          *(u32x4_t*)(lds_x + q * L::kX + i / (SP / 8) * kPitch + i % (SP / 8) * 16) =
+              *(const u32x4_t*)(a.from + q * plane + base + (size_t)b * kThinBlock * SP + i * 8);
+    }
+    __syncthreads();
+    if constexpr (MODE != THIN_FIRST) {
+      // the wave's 16 columns: lane l holds column l % 16 and, of fragment i, rows 16 i + 4 (l / 16) + 0..3
+      const int mine = (16 * wave + in) * kPitch;
+      auto times_h = [&](const char* x, f32x4 (&sum)[NB]) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const int at = (ks * 32 + quad * 8) * 2;
+          const f16x8 xh = *(const f16x8*)(x + mine + at);
+          f16x8 xl;
+          if constexpr (PLANES == 2) xl = *(const f16x8*)(x + L::kX + mine + at);
+#pragma unroll
+          for (int i = 0; i < NB; ++i) {
+            const f16x8 hh = *(const f16x8*)(lds_h + (16 * i + in) * kPitch + at);
+            sum[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hh, xh, sum[i], 0, 0, 0);
+            if constexpr (PLANES == 2) {
+              const f16x8 hl = *(const f16x8*)(lds_h + L::kH + (16 * i + in) * kPitch + at);
+              sum[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hh, xl, sum[i], 0, 0, 0);
+              sum[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hl, xh, sum[i], 0, 0, 0);
+            }
+          }
+        }
+      };
+      auto split = [&](char* to, int i, const f32x4& v) {  // four rows of the lane's column
+        f32x4 w = v;
+        asm("" : "+v"(w));
+        uint2 hi = {pack_f16x2(w[0], w[1]), pack_f16x2(w[2], w[3])};
+        *(uint2*)(to + mine + (16 * i + 4 * quad) * 2) = hi;
+        if constexpr (PLANES == 2) {
+          const f16x2 h0 = unpack_f16x2(hi.x), h1 = unpack_f16x2(hi.y);
+          *(uint2*)(to + L::kX + mine + (16 * i + 4 * quad) * 2) =
+              uint2{pack_f16x2(w[0] - (float)h0.x, w[1] - (float)h0.y), pack_f16x2(w[2] - (float)h1.x, w[3] - (float)h1.y)};
+        }
+      };
+      f32x4 x[NB], y[NB], v[NB];
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        const uint2 hi = *(const uint2*)(lds_x + mine + (16 * i + 4 * quad) * 2);
+        const f16x2 h0 = unpack_f16x2(hi.x), h1 = unpack_f16x2(hi.y);
+        x[i] = f32x4{(float)h0.x, (float)h0.y, (float)h1.x, (float)h1.y};
+        if constexpr (PLANES == 2) {
+          const uint2 lo = *(const uint2*)(lds_x + L::kX + mine + (16 * i + 4 * quad) * 2);
+          const f16x2 l0 = unpack_f16x2(lo.x), l1 = unpack_f16x2(lo.y);
+          x[i] += f32x4{(float)l0.x, (float)l0.y, (float)l1.x, (float)l1.y};
+        }
+        y[i] = v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+      auto rest = [&](int i, const f32x4& w) {  // what one plane of H lacks on its diagonal, times w
+        if constexpr (PLANES == 1) return *(const f32x4*)(lds_r + 16 * i + 4 * quad) * w;
+        else return f32x4{0.f, 0.f, 0.f, 0.f};
+      };
+      times_h(lds_x, y);
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        y[i] = y[i] * (1.f / kOrthoScale) + rest(i, x[i]);
+        split(lds_y, i, y[i]);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");  // the wave's own columns
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      times_h(lds_y, v);
+#pragma unroll
+      for (int i = 0; i < NB; ++i) v[i] = a.q0 * x[i] + a.lin * y[i] + a.c2 * (v[i] * (1.f / kOrthoScale) + rest(i, y[i]));
+      if constexpr (MODE == THIN_STEP) {
+#pragma unroll
+        for (int i = 0; i < NB; ++i) split(lds_x, i, v[i]);
+      } else {
+        __syncthreads();  // X and Y are read; the tile takes their place
+        float* const tile = (float*)lds_x;
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) tile[(16 * wave + in) * (SP + 1) + 16 * i + 4 * quad + e] = v[i][e] * (1.f / kOrthoScale);
+      }
+      __syncthreads();
+    }
+    if constexpr (MODE == THIN_LAST) {
+      float* const tile = (float*)lds_x;
+      // as the matrix lies: consecutive threads, consecutive elements
+      for (int i = tid; i < kThinBlock * SP; i += 256) {
+        const int c = z.tall ? i / SP : i % kThinBlock, r = z.tall ? i % SP : i / kThinBlock, col = b * kThinBlock + c;
+        if (r >= small || col >= large) continue;
+        const size_t at = matrix * elems + (z.tall ? (size_t)col * z.cols + r : (size_t)r * z.cols + col);
+        const float v = tile[c * (SP + 1) + r];
+        if constexpr (UPDATE) {
+          const float w = fmaf(u.keep, u.master[at], -u.rate * v);
+          u.master_out[at] = w;
+          tile[c * (SP + 1) + r] = w;
+        } else {
+          store_elem<Elem>(out + at, v);
+        }
+      }
+      if constexpr (UPDATE) {  // (a thread reads back what it wrote itself)
+        for (int s0 = 0; s0 < u.slots; s0 += 64) {
+          const int s = s0 + lane;
+          unsigned long long set = __ballot(s < u.slots && u.slot_expert[s < u.slots ? s : 0] == (int)matrix);
+          for (; set != 0; set &= set - 1) {
+            Elem* const to = (Elem*)u.slot_weights + (size_t)(s0 + __ffsll((long long)set) - 1) * elems;
+            for (int i = tid; i < kThinBlock * SP; i += 256) {
+              const int c = z.tall ? i / SP : i % kThinBlock, r = z.tall ? i % SP : i / kThinBlock, col = b * kThinBlock + c;
+              if (r < small && col < large) store_elem<Elem>(to + (z.tall ? (size_t)col * z.cols + r : (size_t)r * z.cols + col), tile[c * (SP + 1) + r]);
+            }
+          }
+        }
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < PLANES; ++q)
+        for (int i = tid; i < kThinBlock * SP / 8; i += 256)
+          *(u32x4_t*)(a.to + q * plane + base + (size_t)b * kThinBlock * SP + i * 8) =
+              *(const u32x4_t*)(lds_x + q * L::kX + i / (SP / 8) * kPitch + i % (SP / 8) * 16);
+      // G of the block: both factors are the block's rows, k (its columns) major: transposing reads
+      const int k_row = 8 * quad + (in >> 2);
+      auto rows = [&](int q, int i, int ks) {
+        const char* const p = lds_x + q * L::kX + (ks * 32 + k_row) * kPitch + i * 32 + (in & 3) * 8;
+        const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)p);
+        const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(p + 4 * kPitch));
+        return __builtin_bit_cast(f16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      };
+#pragma unroll
+      for (int t = 0; t < NB * NB / 4; ++t) {
+        const int block = wave * (NB * NB / 4) + t, bi = block / NB, bj = block % NB;
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+        if constexpr (PLANES == 1) sum = gram[t];
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+          const f16x8 ih = rows(0, bi, ks), jh = rows(0, bj, ks);
+          sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(jh, ih, sum, 0, 0, 0);
+          if constexpr (PLANES == 2) {
+            sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(rows(1, bj, ks), ih, sum, 0, 0, 0);
+            sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(jh, rows(1, bi, ks), sum, 0, 0, 0);
+          }
+        }
+        if constexpr (PLANES == 1) gram[t] = sum;
+        else gram[t] += sum;
+      }
+    }
+  }
+  if constexpr (MODE != THIN_LAST) {
+    float* const part = a.part_out + (matrix * a.parts + blockIdx.x) * (SP * SP);
+#pragma unroll
+    for (int t = 0; t < NB * NB / 4; ++t) {
+      const int block = wave * (NB * NB / 4) + t, bi = block / NB, bj = block % NB;
+      *(f32x4*)(part + (16 * bi + in) * SP + 16 * bj + 4 * quad) = gram[t];
+    }
+  }
+#endif
+}
+
+inline int thin_side(int small) { return small <= 32 ? 32 : small <= 64 ? 64 : 128; }
+// Workgroups of a matrix: those that fill the chip twice, a block of columns each at least, and not so many that adding up their parts
+// of G is what they do.
+inline int thin_parts(int n, int columns) {
+  const int fill = (512 + n - 1) / n, blocks = columns / kThinBlock;
+  const int most = fill < blocks ? fill : blocks;
+  return most < kThinMostParts ? most : kThinMostParts;
+}
+
+// Lets a kernel have so much dynamic LDS; once per device (idempotent).
+template <auto KERNEL>
+int32_t thin_lds(int bytes) {
+  static std::atomic<bool> ready_on_device[kMaxDevices];
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return LZ_EHIP;
+  if (!ready_on_device[dev].load(std::memory_order_acquire)) {
+    if (hipFuncSetAttribute((const void*)KERNEL, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return LZ_EHIP;
+    ready_on_device[dev].store(true, std::memory_order_release);
+  }
+  return LZ_OK;
+}
+
+template <typename Elem, bool UPDATE, int MODE, int SP, int PLANES>
+int32_t launch_thin(const ThinArgs& a, const Source& source, const OrthoSize& z, void* out, const Update& u, hipStream_t st) {
+  constexpr auto kern = thin_step_kernel<Elem, UPDATE, MODE, SP, PLANES>;
+  constexpr int kLds = ThinLds<SP, PLANES>::bytes;
+  const int32_t rc = thin_lds<kern>(kLds);
+  if (rc != LZ_OK) return rc;
+  hipLaunchKernelGGL(kern, dim3(a.parts, z.n), dim3(256), kLds, st, a, source, z, (Elem*)out, u);
+  return lz::launch_status();
+}
+
+}  // namespace
