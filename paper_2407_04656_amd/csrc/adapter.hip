@@ -37,6 +37,12 @@ inline int splits_of(const lz_adapter_shape* s, int n_out, int K) {
   const long long fill = 512 / (tiles > 0 ? tiles : 1);
   return (int)(fill < 1 ? 1 : fill < most ? fill : most);
 }
+// Workgroups that share a tile of h: so many that the chip's 512 places are taken, eight K steps at least each.
+inline int low_rank_splits(const lz_adapter_shape* s, int d) {
+  const long long tiles = (long long)ceil_div(s->T, kNarrow) * ceil_div(s->rank, kNarrow), most = ceil_div(ceil_div(d, BK), 8);
+  const long long fill = 512 / (tiles > 0 ? tiles : 1);
+  return (int)(fill < 1 ? 1 : fill < most ? fill : most);
+}
 // Rows of a unit of the factors' gradients.
 inline int factor_chunk(int T) {
   const int even = (T / 16 + 63) / 64 * 64;
@@ -54,7 +60,7 @@ struct AdapterWorkspace {
   void *tiles, *tiles_split;          // row tiles of the adapters' rows
   void *all_tiles, *all_tiles_split;  // of all rows as one slot
   void *xs, *dys;    // x, dy by rows
-  float* low;        // [T, rank] before the scale
+  float* low;        // [T, rank] before the scale; bf16 kernels: of every split
   void* dh;          // [T, rank]
   float* sum;        // [T, max(d_in, d_out)]
   // shapes on the bf16 kernels
@@ -87,7 +93,10 @@ AdapterWorkspace carve(void* ws, const lz_adapter_shape* s) {
   w.all_tiles_split = take(tile_table_bytes(s->T, 1, kSplitRows));
   w.xs = take(eb * T * s->d_in);
   w.dys = take(eb * T * s->d_out);
-  w.low = (float*)take(4 * T * s->rank);
+  {
+    const int in = low_rank_splits(s, s->d_in), out = low_rank_splits(s, s->d_out);
+    w.low = (float*)take(4 * T * s->rank * (whole_pieces(s) ? (in > out ? in : out) : 1));
+  }
   w.dh = take(eb * T * s->rank);
   w.sum = (float*)take(4 * T * d);
   if (whole_pieces(s)) {
@@ -344,11 +353,19 @@ constexpr int kFewTokens = 128;
 
 int32_t low_rank_mfma(const AdapterWorkspace& w, const lz_adapter_shape* s, const void* x, int d, const void* a, const float* scale, void* h,
                       hipStream_t st) {
-  const LowRankArgs args{(const uint16_t*)x, (const uint16_t*)a, scale, w.ids, w.lists.count64, w.lists.list64, w.lists.local64,
-                         (uint16_t*)h, s->T, d, s->rank};
-  if (s->T <= kFewTokens) hipLaunchKernelGGL(low_rank_token_kernel, dim3(s->T, ceil_div(s->rank, 4)), dim3(256), 0, st, args);
-  else if (s->T < 8192) hipLaunchKernelGGL((low_rank_kernel<1>), dim3(ceil_div(s->T, 16)), dim3(512), 0, st, args);
-  else hipLaunchKernelGGL((low_rank_kernel<2>), dim3(ceil_div(s->T, 32)), dim3(512), 0, st, args);
+  LowRankArgs args{(const uint16_t*)x, (const uint16_t*)a, scale, w.ids, w.lists.count64, w.lists.list64, w.lists.local64,
+                   (uint16_t*)h, w.low, s->T, d, s->rank, low_rank_splits(s, d)};
+  if (s->T <= kFewTokens) {
+    hipLaunchKernelGGL(low_rank_token_kernel, dim3(s->T, ceil_div(s->rank, 4)), dim3(256), 0, st, args);
+    return lz::launch_status();
+  }
+  const dim3 grid(ceil_div(s->T, kNarrow) * args.splits, ceil_div(s->rank, kNarrow));
+  if (d % BK != 0) hipLaunchKernelGGL(low_rank_kernel<true>, grid, dim3(256), kNarrowLds, st, args);
+  else hipLaunchKernelGGL(low_rank_kernel<false>, grid, dim3(256), kNarrowLds, st, args);
+  if (args.splits > 1) {
+    const size_t pieces = (size_t)s->T * s->rank / 4;
+    hipLaunchKernelGGL(join_low_rank_kernel, dim3((unsigned)((pieces + 255) / 256)), dim3(256), 0, st, args);
+  }
   return lz::launch_status();
 }
 

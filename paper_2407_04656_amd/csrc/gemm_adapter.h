@@ -11,6 +11,19 @@
 
 namespace {
 
+// Lets a kernel have so much dynamic LDS; once per device (idempotent).
+template <auto KERNEL>
+int32_t allow_lds(int bytes) {
+  static std::atomic<bool> ready_on_device[kMaxDevices];
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return LZ_EHIP;
+  if (!ready_on_device[dev].load(std::memory_order_acquire)) {
+    if (hipFuncSetAttribute((const void*)KERNEL, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return LZ_EHIP;
+    ready_on_device[dev].store(true, std::memory_order_release);
+  }
+  return LZ_OK;
+}
+
 // Which adapters the tokens of 256 and of 64 consecutive rows use, and where in that list each row's stands (255: none).
 struct AdapterLists {
   int32_t *count256, *list256;
@@ -37,18 +50,18 @@ __global__ __launch_bounds__(256) void adapter_lists_kernel(const int32_t* __res
       atomicOr(status, LZ_ADAPTER_BAD_ID);
     }
   }
-  // 64 rows, one wave: adapters in the order in which they occur
+  // 64 rows, one wave: every row looks for the first row with its adapter; those that are the first are the list, in their order
+  // (an adapter after the other, 64 decoding requests took 3 us of them)
   const int block = blockIdx.x * 4 + wave;
-  int place = 255, n64 = 0;
-  for (unsigned long long left = __ballot(id >= 0); left != 0; ++n64) {
-    const int a = __shfl(id, __ffsll((long long)left) - 1);
-    const unsigned long long same = __ballot(id == a);
-    if (id == a) place = n64;
-    if (lane == 0) out.list64[(size_t)block * 64 + n64] = a;
-    left &= ~same;
-  }
+  int leader = lane;
+#pragma unroll 16
+  for (int l = 63; l >= 0; --l)
+    if (__builtin_amdgcn_readlane(id, l) == id) leader = l;
+  const unsigned long long heads = __ballot(id >= 0 && leader == lane);
+  const int place = id >= 0 ? __popcll(heads & ((1ull << leader) - 1)) : 255;
+  if (id >= 0 && leader == lane) out.list64[(size_t)block * 64 + place] = id;
   out.local64[(size_t)block * 64 + lane] = (uint8_t)place;
-  if (lane == 0) out.count64[block] = n64;
+  if (lane == 0) out.count64[block] = __popcll(heads);
   // 256 rows
   __syncthreads();
   if (id >= 0) atomicMin(&first[id], tid);
@@ -79,7 +92,8 @@ struct LowRankArgs {
   const int32_t *count64, *list64;
   const uint8_t* local64;
   uint16_t* h;  // [T, rank]
-  int T, d, rank;
+  float* part;  // [splits, T, rank]
+  int T, d, rank, splits;
 };
 
 __device__ __forceinline__ bf16x8 load_bf16x8(const uint16_t* p) { return *(const bf16x8*)p; }
@@ -93,11 +107,20 @@ __global__ __launch_bounds__(256) void low_rank_token_kernel(LowRankArgs a) {
   if (id >= 0) {
     const uint16_t* const x = a.x + (size_t)t * a.d;
     const uint16_t* const w = a.a + ((size_t)id * a.rank + r) * a.d;
-#pragma unroll 4
-    for (int k = lane * 8; k < a.d; k += 512) {
-      const bf16x8 u = load_bf16x8(x + k), v = load_bf16x8(w + k);
+    constexpr int kAhead = 8;  // pieces of either in flight: one trip to memory up to 4096 columns
+    for (int k0 = lane * 8; k0 < a.d; k0 += 512 * kAhead) {
+      bf16x8 u[kAhead], v[kAhead];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sum = fmaf((float)u[j], (float)v[j], sum);
+      for (int i = 0; i < kAhead; ++i) {
+        const int k = k0 + 512 * i < a.d ? k0 + 512 * i : k0;
+        u[i] = load_bf16x8(x + k);
+        v[i] = load_bf16x8(w + k);
+      }
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i)
+        if (k0 + 512 * i < a.d)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) sum = fmaf((float)u[i][j], (float)v[i][j], sum);
     }
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
@@ -106,82 +129,119 @@ __global__ __launch_bounds__(256) void low_rank_token_kernel(LowRankArgs a) {
   if (lane == 0) a.h[(size_t)t * a.rank + r] = lz::f32_to_bf16(sum);
 }
 
-// 16 RT tokens a workgroup, 64 columns of h at a time, for every adapter among the tokens.  Eight waves take every eighth 64 k of
-// the sum each, from global memory to the registers (nothing is used twice but by the other fragments of the wave), and add up
-// through LDS.  Bound by reading x once.
-template <int RT>
-__global__ __launch_bounds__(512) void low_rank_kernel(LowRankArgs a) {
+// 64 tokens x 64 columns of h: the ring of gemm_narrow.h over the K steps of one adapter of the tile's list after the other, whose rows
+// are stored when its last step is done.  Bound by reading x (a second adapter's pass finds it in the cache), so that the sum over
+// K is split among workgroups where tiles are few.  Fragments straight from memory to registers, 16 rows of 64 bytes a load, took
+// 50 us for 8192 tokens of 2048 and of 8192 columns (mean) where this takes 30, and more the more waves were there: every half line
+// was fetched by itself.
+// blockIdx.x = tile x split, blockIdx.y = columns.
+template <bool KTAIL>
+__global__ __launch_bounds__(256, 2) void low_rank_kernel(LowRankArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  constexpr int kRows = 16 * RT;
-  __shared__ float part[8][kRows][64 + 4];
+  constexpr int NS = kNarrowStages, kLoads = 4;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int tile = blockIdx.x / a.splits, split = blockIdx.x % a.splits, row0 = tile * kNarrow, r0 = blockIdx.y * kNarrow;
+  const int n_rows = a.T - row0 < kNarrow ? a.T - row0 : kNarrow, K = a.d;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int t0 = blockIdx.x * kRows, block = t0 / 64, frag = lane & 15, quad = lane >> 4;
-  const int mine = lane < kRows ? a.local64[(size_t)t0 + lane] : 255;  // (rows past T: 255)
-  for (int i = threadIdx.x; i < kRows * a.rank; i += 512)
-    if (a.local64[(size_t)t0 + i / a.rank] == 255 && t0 + i / a.rank < a.T) a.h[(size_t)t0 * a.rank + i] = 0;
-  const uint16_t* xrow[RT];
+  const int wm = wave >> 1, wn = wave & 1;
+  const int count = __builtin_amdgcn_readfirstlane(a.count64[tile]);
+  const int32_t* const list = a.list64 + (size_t)tile * 64;
+  const uint8_t* const local = a.local64 + (size_t)tile * 64;
+  const int all = (K + BK - 1) / BK, first = (int)((long long)all * split / a.splits), each = (int)((long long)all * (split + 1) / a.splits) - first;
+  const i32x4 wordsX = rsrc_words(a.x + (size_t)row0 * K, (uint32_t)n_rows * (uint32_t)K * 2u), wordsNull = rsrc_words(a.x, 0);
+  const uint32_t factor_bytes = (uint32_t)(a.rank - r0) * (uint32_t)K * 2u;  // rows past the rank: zeros, no traffic
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
+  int voff[2];
+  [[maybe_unused]] int tail_or[2] = {0, 0};
 #pragma unroll
-  for (int j = 0; j < RT; ++j) {
-    const int t = t0 + j * 16 + frag;
-    xrow[j] = a.x + (size_t)(t < a.T ? t : a.T - 1) * a.d;
+  for (int i = 0; i < 2; ++i) {
+    const int r = (wave * 2 + i) * 8 + (lane >> 3), chunk = ((lane & 7) ^ swz(r)) * 8;
+    voff[i] = (int)(((uint32_t)r * (uint32_t)K + (uint32_t)chunk) * 2u);
+    if (KTAIL && chunk >= K - (all - 1) * BK) tail_or[i] = (int)0x80000000;
   }
-  const bf16x8 none = {};
-  const int count = a.count64[block];
-  for (int e = 0; e < count; ++e) {
-    if (__ballot(mine == e) == 0) continue;  // the same in every wave
-    const int id = __builtin_amdgcn_readfirstlane(a.list64[(size_t)block * 64 + e]);
-    const float scale = a.scale[id];
-    for (int r0 = 0; r0 < a.rank; r0 += 64) {
-      const int frags = (a.rank - r0 + 15) / 16 < 4 ? (a.rank - r0 + 15) / 16 : 4;
-      f32x4 acc[4][RT] = {};
-      auto sum = [&](auto n_frags) {
-        constexpr int NF = decltype(n_frags)::value;
-        const uint16_t* arow[NF];
-        bool in[NF];
+  // the next step to load: which adapter, which of its steps
+  int load_e = 0, load_k = 0;
+  const uint16_t* factor = count > 0 ? a.a + ((size_t)__builtin_amdgcn_readfirstlane(list[0]) * a.rank + r0) * K : nullptr;
+  auto issue = [&](int stage) {  // past the end: zeros, without memory traffic
+    const bool real = load_e < count;
+    const i32x4 wx = real ? wordsX : wordsNull, wa = rsrc_words(factor, real ? factor_bytes : 0);
+    const uint32_t lds = lds0 + stage * kNarrowStage;
+    const int step = first + load_k, tail = step == all - 1 ? -1 : 0;
 #pragma unroll
-        for (int f = 0; f < NF; ++f) {
-          in[f] = r0 + f * 16 + frag < a.rank;
-          arow[f] = a.a + ((size_t)id * a.rank + (in[f] ? r0 + f * 16 + frag : r0)) * a.d;
-        }
-#pragma clang loop unroll_count(2)
-        for (int k = wave * 64; k < a.d; k += 512) {
+    for (int i = 0; i < 2; ++i) load16_to_lds(wa, lds + kNarrowOperand + (wave * 2 + i) * 1024, KTAIL ? voff[i] | (tail_or[i] & tail) : voff[i], step * BK * 2);
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            const int at = k + half * 32 + quad * 8;
-            const bool ok = at < a.d;
-            bf16x8 x[RT], w[NF];
-#pragma unroll
-            for (int j = 0; j < RT; ++j) x[j] = ok ? load_bf16x8(xrow[j] + at) : none;
-#pragma unroll
-            for (int f = 0; f < NF; ++f) w[f] = ok && in[f] ? load_bf16x8(arow[f] + at) : none;
-#pragma unroll
-            for (int f = 0; f < NF; ++f)
-#pragma unroll
-              for (int j = 0; j < RT; ++j) acc[f][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[f], x[j], acc[f][j], 0, 0, 0);
-          }
-        }
-      };
-      if (frags == 1) sum(std::integral_constant<int, 1>{});
-      else if (frags == 2) sum(std::integral_constant<int, 2>{});
-      else sum(std::integral_constant<int, 4>{});
-#pragma unroll
-      for (int f = 0; f < 4; ++f)
-#pragma unroll
-        for (int j = 0; j < RT; ++j)
-          if (f < frags) *(f32x4*)&part[wave][j * 16 + frag][f * 16 + 4 * quad] = acc[f][j];
-      __syncthreads();
-      const int cols = frags * 16;
-      for (int i = threadIdx.x; i < kRows * cols; i += 512) {
-        const int r = i / cols, c = i - r * cols;
-        float s = 0.f;
-#pragma unroll
-        for (int w = 0; w < 8; ++w) s += part[w][r][c];
-        if (a.local64[(size_t)t0 + r] == e && r0 + c < a.rank) a.h[(size_t)(t0 + r) * a.rank + r0 + c] = lz::f32_to_bf16(scale * s);
-      }
-      __syncthreads();
+    for (int i = 0; i < 2; ++i) load16_to_lds(wx, lds + (wave * 2 + i) * 1024, KTAIL ? voff[i] | (tail_or[i] & tail) : voff[i], step * BK * 2);
+    if (++load_k == each) {
+      load_k = 0;
+      if (++load_e < count) factor = a.a + ((size_t)__builtin_amdgcn_readfirstlane(list[load_e]) * a.rank + r0) * K;
     }
+  };
+  int fragoff[2];
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks) fragoff[ks] = (lane & 15) * kRowBytes + (((ks * 4 + (lane >> 4)) ^ swz(lane & 15)) << 4);
+  // the lane's rows: 32 wm + 16 j + lane % 16
+  int place[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) place[j] = local[32 * wm + 16 * j + (lane & 15)];  // (rows past T: none)
+  auto store = [&](int j, int c, const f32x4& v, float scale) {
+    const int col = r0 + 32 * wn + 16 * c + 4 * (lane >> 4), t = row0 + 32 * wm + 16 * j + (lane & 15);
+    if (col >= a.rank || t >= a.T) return;  // a rank is whole 8s
+    if (a.splits > 1) *(f32x4*)(a.part + ((size_t)split * a.T + t) * a.rank + col) = v;
+    else *(uint2*)(a.h + (size_t)t * a.rank + col) = uint2{pack_bf16x2(scale * v[0], scale * v[1]), pack_bf16x2(scale * v[2], scale * v[3])};
+  };
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+      if (place[j] == 255) store(j, c, f32x4{0.f, 0.f, 0.f, 0.f}, 0.f);
+  f32x4 acc[2][2] = {};
+#pragma unroll
+  for (int s = 0; s < NS - 1; ++s) issue(s);
+  int stage = 0;
+  for (int e = 0; e < count; ++e) {
+    const float scale = a.scale[__builtin_amdgcn_readfirstlane(list[e])];
+    for (int kt = 0; kt < each; ++kt) {
+      constexpr int kAhead = (NS - 2) * kLoads;
+      __builtin_amdgcn_s_waitcnt(0x0F70 | (kAhead & 15) | ((kAhead >> 4) << 14));  // this wave's loads of the step are in LDS
+      __syncthreads();  // ... everyone's are; and nobody reads the stage before any more
+      issue(stage == 0 ? NS - 1 : stage - 1);
+      const char* const st = smem + stage * kNarrowStage;
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        bf16x8 x[2], w[2];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) w[c] = *(const bf16x8*)(st + kNarrowOperand + (2 * wn + c) * 16 * kRowBytes + fragoff[ks]);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) x[j] = *(const bf16x8*)(st + (2 * wm + j) * 16 * kRowBytes + fragoff[ks]);
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) acc[c][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[c], x[j], acc[c][j], 0, 0, 0);
+      }
+      stage = stage + 1 == NS ? 0 : stage + 1;
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        if (place[j] == e) store(j, c, acc[c][j], scale);
+        acc[c][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
   }
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // the trailing loads are done with LDS
 #endif
+}
+
+// The splits' sums, in their order, scaled.
+__global__ __launch_bounds__(256) void join_low_rank_kernel(LowRankArgs a) {
+  const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4, elems = (size_t)a.T * a.rank;
+  if (i >= elems) return;
+  const int id = a.ids[i / a.rank];  // a rank is whole 8s
+  f32x4 v = {};
+#pragma unroll 4
+  for (int s = 0; s < a.splits; ++s) v += *(const f32x4*)(a.part + s * elems + i);
+  const float scale = id >= 0 ? a.scale[id] : 0.f;
+  *(uint2*)(a.h + i) = uint2{pack_bf16x2(scale * v[0], scale * v[1]), pack_bf16x2(scale * v[2], scale * v[3])};
 }
 
 // ---- the projection on 64 x 64 tiles, the sum over K split among workgroups where tiles are few
@@ -212,8 +272,6 @@ __global__ __launch_bounds__(256, 2) void adapter_narrow_kernel(AdapterNarrowArg
   const int n_rows = a.T - row0 < kNarrow ? a.T - row0 : kNarrow;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1;
-  const int count = __builtin_amdgcn_readfirstlane(a.count64[row_tile]);
-  if (threadIdx.x < 64) list[threadIdx.x] = (int)threadIdx.x < count ? a.list64[(size_t)row_tile * 64 + threadIdx.x] : 0;
 
   const int ldw = TB ? a.n_out : K;
   const i32x4 wordsA = rsrc_words(a.A + (size_t)row0 * K, (uint32_t)n_rows * (uint32_t)K * 2u);
@@ -231,7 +289,6 @@ __global__ __launch_bounds__(256, 2) void adapter_narrow_kernel(AdapterNarrowArg
     const int r = (wave * 2 + i) * 8 + (lane >> 3);
     row[i] = r;
     chunk[i] = ((lane & 7) ^ swz(r)) * 8;
-    local[i] = r < n_rows ? a.local64[(size_t)row0 + r] : 255;
     voffX[i] = (int)(((uint32_t)r * (uint32_t)K + (uint32_t)chunk[i]) * 2u);  // rows past the end lie beyond the descriptor: zeros
     if constexpr (TB) {
       kr[i] = r;
@@ -248,33 +305,11 @@ __global__ __launch_bounds__(256, 2) void adapter_narrow_kernel(AdapterNarrowArg
 #pragma unroll
     for (int i = 0; i < 2; ++i) tail_or[i] = chunk[i] >= k_left ? (int)0x80000000 : 0;
   }
-  const int all_steps = base_steps + (count + per - 1) / per * steps_each;
-  const int begin = (int)((long long)all_steps * split / a.splits), end = (int)((long long)all_steps * (split + 1) / a.splits);
-  __syncthreads();  // the list
-  auto issue = [&](int step, int stage) {  // a step past the end writes zeros, without memory traffic
+  // A workgroup has its share of either kind of steps: what the base's first loads need is known before the list has arrived.
+  auto share = [&](int steps, int nth) { return (int)((long long)steps * nth / a.splits); };
+  const int base0 = share(base_steps, split), n_base = share(base_steps, split + 1) - base0;
+  auto issue_base = [&](int step, int stage, bool real) {  // no step: zeros, without memory traffic
     const uint32_t lds = lds0 + stage * kNarrowStage;
-    if (step >= base_steps && step < end) {
-      const int q = step - base_steps, e0 = q / steps_each * per, k0 = q % steps_each * 64;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int in = rank <= 64 ? kr[i] / rank : 0, k = k0 + kr[i] - in * rank, e = e0 + in;
-        const bool ok = in < per && e < count && k < rank;
-        const int id = list[ok ? e : 0];
-        int voff;
-        if constexpr (TB) voff = ((id * rank + k) * a.n_out + n0 + ((lane & 7) ^ swz_narrow(row[i])) * 8) * 2;
-        else voff = ((id * a.n_out + n0 + row[i]) * rank + k) * 2;
-        // (columns past n_out fetch what lies behind: never stored)
-        load16_to_lds(wordsB, lds + kNarrowOperand + (wave * 2 + i) * 1024, ok ? voff : (int)0x80000000, 0);
-      }
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int in = rank <= 64 ? chunk[i] / rank : 0, k = k0 + chunk[i] - in * rank, e = e0 + in;
-        const bool ok = in < per && e < count && k < rank && local[i] == e;
-        load16_to_lds(wordsH, lds + (wave * 2 + i) * 1024, ok ? (row[i] * rank + k) * 2 : (int)0x80000000, 0);
-      }
-      return;
-    }
-    const bool real = step < end;
     const i32x4 wa = real ? wordsA : wordsNull, ww = real ? wordsW : wordsNull;
     const int tail = step == base_steps - 1 ? -1 : 0;
 #pragma unroll
@@ -288,6 +323,40 @@ __global__ __launch_bounds__(256, 2) void adapter_narrow_kernel(AdapterNarrowArg
       int voff = voffX[i];
       if constexpr (KTAIL) voff |= tail_or[i] & tail;
       load16_to_lds(wa, lds + (wave * 2 + i) * 1024, voff, real ? step * BK * 2 : 0);
+    }
+  };
+#pragma unroll
+  for (int s = 0; s < NS - 1; ++s)
+    if (s < n_base) issue_base(base0 + s, s, true);  // (the others' turn comes below, in order)
+  const int count = __builtin_amdgcn_readfirstlane(a.count64[row_tile]);
+  if (threadIdx.x < 64) list[threadIdx.x] = (int)threadIdx.x < count ? a.list64[(size_t)row_tile * 64 + threadIdx.x] : 0;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) local[i] = row[i] < n_rows ? a.local64[(size_t)row0 + row[i]] : 255;
+  const int low_steps = (count + per - 1) / per * steps_each, low0 = share(low_steps, split), end = n_base + share(low_steps, split + 1) - low0;
+  __syncthreads();  // the list
+  auto issue = [&](int nth, int stage) {
+    if (nth < n_base || nth >= end) {
+      issue_base(base0 + nth, stage, nth < end);
+      return;
+    }
+    const uint32_t lds = lds0 + stage * kNarrowStage;
+    const int q = low0 + nth - n_base, e0 = q / steps_each * per, k0 = q % steps_each * 64;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int in = rank <= 64 ? kr[i] / rank : 0, k = k0 + kr[i] - in * rank, e = e0 + in;
+      const bool ok = in < per && e < count && k < rank;
+      const int id = list[ok ? e : 0];
+      int voff;
+      if constexpr (TB) voff = ((id * rank + k) * a.n_out + n0 + ((lane & 7) ^ swz_narrow(row[i])) * 8) * 2;
+      else voff = ((id * a.n_out + n0 + row[i]) * rank + k) * 2;
+      // (columns past n_out fetch what lies behind: never stored)
+      load16_to_lds(wordsB, lds + kNarrowOperand + (wave * 2 + i) * 1024, ok ? voff : (int)0x80000000, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int in = rank <= 64 ? chunk[i] / rank : 0, k = k0 + chunk[i] - in * rank, e = e0 + in;
+      const bool ok = in < per && e < count && k < rank && local[i] == e;
+      load16_to_lds(wordsH, lds + (wave * 2 + i) * 1024, ok ? (row[i] * rank + k) * 2 : (int)0x80000000, 0);
     }
   };
   int fragoff[2], woff[2];
@@ -318,9 +387,10 @@ __global__ __launch_bounds__(256, 2) void adapter_narrow_kernel(AdapterNarrowArg
   };
   f32x4 acc[2][2] = {};
 #pragma unroll
-  for (int s = 0; s < NS - 1; ++s) issue(begin + s, s);
+  for (int s = 0; s < NS - 1; ++s)
+    if (s >= n_base) issue(s, s);
   int stage = 0;
-  for (int kt = begin; kt < end; ++kt) {
+  for (int kt = 0; kt < end; ++kt) {
     constexpr int kAhead = (NS - 2) * kLoads;
     __builtin_amdgcn_s_waitcnt(0x0F70 | (kAhead & 15) | ((kAhead >> 4) << 14));  // this wave's loads of step kt are in LDS
     __syncthreads();  // ... everyone's are; and nobody reads the stage of step kt - 1 any more
@@ -379,19 +449,6 @@ __global__ __launch_bounds__(256) void join_splits_kernel(const float* __restric
     v1 += *(const f32x4*)(part + s * elems + i + 4);
   }
   *(u32x4_t*)(out + i) = u32x4_t{pack_bf16x2(v0[0], v0[1]), pack_bf16x2(v0[2], v0[3]), pack_bf16x2(v1[0], v1[1]), pack_bf16x2(v1[2], v1[3])};
-}
-
-// Lets a kernel have so much dynamic LDS; once per device (idempotent).
-template <auto KERNEL>
-int32_t allow_lds(int bytes) {
-  static std::atomic<bool> ready_on_device[kMaxDevices];
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return LZ_EHIP;
-  if (!ready_on_device[dev].load(std::memory_order_acquire)) {
-    if (hipFuncSetAttribute((const void*)KERNEL, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return LZ_EHIP;
-    ready_on_device[dev].store(true, std::memory_order_release);
-  }
-  return LZ_OK;
 }
 
 template <int MODE>

@@ -83,12 +83,17 @@ struct ThinLds {
   static constexpr int x = PLANES * kH, y = x + PLANES * kX, r = x + (2 * PLANES * kX > kTile ? 2 * PLANES * kX : kTile), bytes = r + SP * 4;
 };
 
+// Four waves of 16 columns each, for 128 rows eight: either four then has half of the rows of Y and X'.
+template <int SP>
+constexpr int kThinThreads = SP == 128 ? 512 : 256;
+
 // blockIdx.x = part of the columns, blockIdx.y = matrix
 template <typename Elem, bool UPDATE, int MODE, int SP, int PLANES>
-__global__ __launch_bounds__(256) void thin_step_kernel(ThinArgs a, Source source, OrthoSize z, Elem* __restrict__ out, Update u) {
+__global__ __launch_bounds__(kThinThreads<SP>) void thin_step_kernel(ThinArgs a, Source source, OrthoSize z, Elem* __restrict__ out, Update u) {
 #if defined(__HIP_DEVICE_COMPILE__)
   using L = ThinLds<SP, PLANES>;
-  constexpr int kPitch = L::kPitch, NB = SP / 16, KS = SP / 32;
+  constexpr int kPitch = L::kPitch, NB = SP / 16, KS = SP / 32, kThreads = kThinThreads<SP>, kWaves = kThreads / 64;
+  constexpr int NR = NB * 4 / kWaves, kGram = NB * NB / kWaves;  // fragments of rows, blocks of G of a wave
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   char* const lds_h = smem;
   char* const lds_x = smem + L::x;
@@ -99,44 +104,78 @@ __global__ __launch_bounds__(256) void thin_step_kernel(ThinArgs a, Source sourc
   const size_t matrix = blockIdx.y;
   const size_t plane = (size_t)z.n * a.columns * SP, base = matrix * a.columns * SP;
   const size_t elems = (size_t)z.rows * z.cols;
+  const int blocks = a.columns / kThinBlock;
+  const int first = (int)((long long)blocks * blockIdx.x / a.parts), last = (int)((long long)blocks * (blockIdx.x + 1) / a.parts);
+  // a block's elements (FIRST) or pieces of X, fetched while the block before is worked on
+  constexpr int kElems = kThinBlock * SP / kThreads, kParts8 = kElems / 8;
+  float raw[MODE == THIN_FIRST ? kElems : 1];
+  u32x4_t pieces[MODE == THIN_FIRST ? 1 : PLANES * kParts8];
+  auto place = [&](int k, int& c, int& r) {  // element k of the thread: consecutive threads, consecutive elements of the matrix as it lies
+    const int i = tid + kThreads * k;
+    c = z.tall ? i / SP : i % kThinBlock, r = z.tall ? i % SP : i / kThinBlock;
+  };
+  auto fetch = [&](int b) {
+    if constexpr (MODE == THIN_FIRST) {
+#pragma unroll
+      for (int k = 0; k < kElems; ++k) {
+        int c, r;
+        place(k, c, r);
+        const int col = b * kThinBlock + c;
+        raw[k] = 0.f;
+        if (r < small && col < large)
+          raw[k] = source_value<Elem, UPDATE>(source, matrix * elems + (z.tall ? (size_t)col * z.cols + r : (size_t)r * z.cols + col));
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < PLANES; ++q)
+#pragma unroll
+        for (int k = 0; k < kParts8; ++k)
+          pieces[q * kParts8 + k] = *(const u32x4_t*)(a.from + q * plane + base + (size_t)b * kThinBlock * SP + (tid + kThreads * k) * 8);
+    }
+  };
+  if (first < last) fetch(first);
   float inv = 0.f;
   if constexpr (MODE == THIN_FIRST) {
     inv = inverse_norm(a.sums + matrix * a.norm_blocks, a.norm_blocks, a.eps);
   } else {
     // H from the parts of G (at 2^28 times its size)
     const float* const part = a.part_in + matrix * a.parts * (SP * SP);
-    for (int i = tid; i < SP * SP / 8; i += 256) {
-      float v[8] = {};
-      for (int p = 0; p < a.parts; ++p) {
-        const f32x4 v0 = *(const f32x4*)(part + (size_t)p * (SP * SP) + i * 8), v1 = *(const f32x4*)(part + (size_t)p * (SP * SP) + i * 8 + 4);
+    // (several pieces of several parts at a time: one after the other, a launch of 4 parts of 128 x 128 waits 20 us for them)
+    constexpr int kPieces = SP * SP / 8, kAtOnce = kPieces >= kThreads ? kPieces / kThreads : 1;
+    for (int i0 = tid; i0 < kPieces; i0 += kThreads * kAtOnce) {
+      f32x4 sum[kAtOnce][2] = {};
+#pragma clang loop unroll_count(SP == 32 ? 16 : SP == 64 ? 8 : 4)
+      for (int p = 0; p < a.parts; ++p)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] += v0[e], v[e + 4] += v1[e];
-      }
-      const int row = i / (SP / 8), col = i % (SP / 8) * 8;
-      f16x8 hi, lo;
+        for (int k = 0; k < kAtOnce; ++k)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float h = fmaf(v[e], 1.f / kOrthoScale, row == col + e ? -a.mu * kOrthoScale : 0.f);
-        asm("" : "+v"(h));  // rounded to fp32 before it is to fp16, for both parts
-        hi[e] = (_Float16)h;
-        lo[e] = (_Float16)(h - (float)hi[e]);
-        if (PLANES == 1 && row == col + e) lds_r[row] = (h - (float)hi[e]) * (1.f / kOrthoScale);
+          for (int half = 0; half < 2; ++half) sum[k][half] += *(const f32x4*)(part + (size_t)p * (SP * SP) + (i0 + kThreads * k) * 8 + half * 4);
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        const int i = i0 + kThreads * k, row = i / (SP / 8), col = i % (SP / 8) * 8;
+        f16x8 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float h = fmaf(sum[k][e / 4][e % 4], 1.f / kOrthoScale, row == col + e ? -a.mu * kOrthoScale : 0.f);
+          asm("" : "+v"(h));  // rounded to fp32 before it is to fp16, for both parts
+          hi[e] = (_Float16)h;
+          lo[e] = (_Float16)(h - (float)hi[e]);
+          if (PLANES == 1 && row == col + e) lds_r[row] = (h - (float)hi[e]) * (1.f / kOrthoScale);
+        }
+        *(f16x8*)(lds_h + row * kPitch + col * 2) = hi;
+        if constexpr (PLANES == 2) *(f16x8*)(lds_h + L::kH + row * kPitch + col * 2) = lo;
       }
-      *(f16x8*)(lds_h + row * kPitch + col * 2) = hi;
-      if constexpr (PLANES == 2) *(f16x8*)(lds_h + L::kH + row * kPitch + col * 2) = lo;
     }
   }
-  f32x4 gram[NB * NB / 4] = {};
-  const int blocks = a.columns / kThinBlock;
-  const int first = (int)((long long)blocks * blockIdx.x / a.parts), last = (int)((long long)blocks * (blockIdx.x + 1) / a.parts);
+  f32x4 gram[kGram] = {};
   for (int b = first; b < last; ++b) {
     __syncthreads();  // H is there; nobody reads the last block any more
     if constexpr (MODE == THIN_FIRST) {
-      for (int i = tid; i < kThinBlock * SP; i += 256) {
-        const int c = z.tall ? i / SP : i % kThinBlock, r = z.tall ? i % SP : i / kThinBlock, col = b * kThinBlock + c;
-        float v = 0.f;
-        if (r < small && col < large)
-          v = source_value<Elem, UPDATE>(source, matrix * elems + (z.tall ? (size_t)col * z.cols + r : (size_t)r * z.cols + col)) * inv * kOrthoScale;
+#pragma unroll
+      for (int k = 0; k < kElems; ++k) {
+        int c, r;
+        place(k, c, r);
+        float v = raw[k] * inv * kOrthoScale;
         asm("" : "+v"(v));
         const _Float16 hi = (_Float16)v;
         *(_Float16*)(lds_x + c * kPitch + r * 2) = hi;
@@ -145,15 +184,18 @@ __global__ __launch_bounds__(256) void thin_step_kernel(ThinArgs a, Source sourc
     } else {
 #pragma unroll
       for (int q = 0; q < PLANES; ++q)
-        for (int i = tid; i < kThinBlock * SP / 8; i += 256)
-          *(u32x4_t*)(lds_x + q * L::kX + i / (SP / 8) * kPitch + i % (SP / 8) * 16) =
-              *(const u32x4_t*)(a.from + q * plane + base + (size_t)b * kThinBlock * SP + i * 8);
+#pragma unroll
+        for (int k = 0; k < kParts8; ++k) {
+          const int i = tid + kThreads * k;
+          *(u32x4_t*)(lds_x + q * L::kX + i / (SP / 8) * kPitch + i % (SP / 8) * 16) = pieces[q * kParts8 + k];
+        }
     }
+    if (b + 1 < last) fetch(b + 1);
     __syncthreads();
     if constexpr (MODE != THIN_FIRST) {
-      // the wave's 16 columns: lane l holds column l % 16 and, of fragment i, rows 16 i + 4 (l / 16) + 0..3
-      const int mine = (16 * wave + in) * kPitch;
-      auto times_h = [&](const char* x, f32x4 (&sum)[NB]) {
+      // the wave's 16 columns: lane l holds column l % 16 and, of fragment i, rows 16 (i0 + i) + 4 (l / 16) + 0..3
+      const int col_in = 16 * (wave & 3) + in, mine = col_in * kPitch, i0 = (wave >> 2) * NR;
+      auto times_h = [&](const char* x, f32x4 (&sum)[NR]) {
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
           const int at = (ks * 32 + quad * 8) * 2;
@@ -161,11 +203,11 @@ __global__ __launch_bounds__(256) void thin_step_kernel(ThinArgs a, Source sourc
           f16x8 xl;
           if constexpr (PLANES == 2) xl = *(const f16x8*)(x + L::kX + mine + at);
 #pragma unroll
-          for (int i = 0; i < NB; ++i) {
-            const f16x8 hh = *(const f16x8*)(lds_h + (16 * i + in) * kPitch + at);
+          for (int i = 0; i < NR; ++i) {
+            const f16x8 hh = *(const f16x8*)(lds_h + (16 * (i0 + i) + in) * kPitch + at);
             sum[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hh, xh, sum[i], 0, 0, 0);
             if constexpr (PLANES == 2) {
-              const f16x8 hl = *(const f16x8*)(lds_h + L::kH + (16 * i + in) * kPitch + at);
+              const f16x8 hl = *(const f16x8*)(lds_h + L::kH + (16 * (i0 + i) + in) * kPitch + at);
               sum[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hh, xl, sum[i], 0, 0, 0);
               sum[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hl, xh, sum[i], 0, 0, 0);
             }
@@ -176,90 +218,91 @@ __global__ __launch_bounds__(256) void thin_step_kernel(ThinArgs a, Source sourc
         f32x4 w = v;
         asm("" : "+v"(w));
         uint2 hi = {pack_f16x2(w[0], w[1]), pack_f16x2(w[2], w[3])};
-        *(uint2*)(to + mine + (16 * i + 4 * quad) * 2) = hi;
+        *(uint2*)(to + mine + (16 * (i0 + i) + 4 * quad) * 2) = hi;
         if constexpr (PLANES == 2) {
           const f16x2 h0 = unpack_f16x2(hi.x), h1 = unpack_f16x2(hi.y);
-          *(uint2*)(to + L::kX + mine + (16 * i + 4 * quad) * 2) =
+          *(uint2*)(to + L::kX + mine + (16 * (i0 + i) + 4 * quad) * 2) =
               uint2{pack_f16x2(w[0] - (float)h0.x, w[1] - (float)h0.y), pack_f16x2(w[2] - (float)h1.x, w[3] - (float)h1.y)};
         }
       };
-      f32x4 x[NB], y[NB], v[NB];
+      f32x4 x[NR], y[NR], v[NR];
 #pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        const uint2 hi = *(const uint2*)(lds_x + mine + (16 * i + 4 * quad) * 2);
+      for (int i = 0; i < NR; ++i) {
+        const uint2 hi = *(const uint2*)(lds_x + mine + (16 * (i0 + i) + 4 * quad) * 2);
         const f16x2 h0 = unpack_f16x2(hi.x), h1 = unpack_f16x2(hi.y);
         x[i] = f32x4{(float)h0.x, (float)h0.y, (float)h1.x, (float)h1.y};
         if constexpr (PLANES == 2) {
-          const uint2 lo = *(const uint2*)(lds_x + L::kX + mine + (16 * i + 4 * quad) * 2);
+          const uint2 lo = *(const uint2*)(lds_x + L::kX + mine + (16 * (i0 + i) + 4 * quad) * 2);
           const f16x2 l0 = unpack_f16x2(lo.x), l1 = unpack_f16x2(lo.y);
           x[i] += f32x4{(float)l0.x, (float)l0.y, (float)l1.x, (float)l1.y};
         }
         y[i] = v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
       auto rest = [&](int i, const f32x4& w) {  // what one plane of H lacks on its diagonal, times w
-        if constexpr (PLANES == 1) return *(const f32x4*)(lds_r + 16 * i + 4 * quad) * w;
+        if constexpr (PLANES == 1) return *(const f32x4*)(lds_r + 16 * (i0 + i) + 4 * quad) * w;
         else return f32x4{0.f, 0.f, 0.f, 0.f};
       };
       times_h(lds_x, y);
 #pragma unroll
-      for (int i = 0; i < NB; ++i) {
+      for (int i = 0; i < NR; ++i) {
         y[i] = y[i] * (1.f / kOrthoScale) + rest(i, x[i]);
         split(lds_y, i, y[i]);
       }
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");  // the wave's own columns
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      __syncthreads();  // Y is there; nobody reads X any more
       times_h(lds_y, v);
 #pragma unroll
-      for (int i = 0; i < NB; ++i) v[i] = a.q0 * x[i] + a.lin * y[i] + a.c2 * (v[i] * (1.f / kOrthoScale) + rest(i, y[i]));
+      for (int i = 0; i < NR; ++i) v[i] = a.q0 * x[i] + a.lin * y[i] + a.c2 * (v[i] * (1.f / kOrthoScale) + rest(i, y[i]));
       if constexpr (MODE == THIN_STEP) {
 #pragma unroll
-        for (int i = 0; i < NB; ++i) split(lds_x, i, v[i]);
+        for (int i = 0; i < NR; ++i) split(lds_x, i, v[i]);
       } else {
-        __syncthreads();  // X and Y are read; the tile takes their place
+        __syncthreads();  // Y is read; the tile takes the place of both
         float* const tile = (float*)lds_x;
 #pragma unroll
-        for (int i = 0; i < NB; ++i)
+        for (int i = 0; i < NR; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) tile[(16 * wave + in) * (SP + 1) + 16 * i + 4 * quad + e] = v[i][e] * (1.f / kOrthoScale);
+          for (int e = 0; e < 4; ++e) tile[col_in * (SP + 1) + 16 * (i0 + i) + 4 * quad + e] = v[i][e] * (1.f / kOrthoScale);
       }
       __syncthreads();
     }
     if constexpr (MODE == THIN_LAST) {
       float* const tile = (float*)lds_x;
-      // as the matrix lies: consecutive threads, consecutive elements
-      for (int i = tid; i < kThinBlock * SP; i += 256) {
-        const int c = z.tall ? i / SP : i % kThinBlock, r = z.tall ? i % SP : i / kThinBlock, col = b * kThinBlock + c;
-        if (r >= small || col >= large) continue;
-        const size_t at = matrix * elems + (z.tall ? (size_t)col * z.cols + r : (size_t)r * z.cols + col);
-        const float v = tile[c * (SP + 1) + r];
-        if constexpr (UPDATE) {
-          const float w = fmaf(u.keep, u.master[at], -u.rate * v);
-          u.master_out[at] = w;
-          tile[c * (SP + 1) + r] = w;
-        } else {
-          store_elem<Elem>(out + at, v);
+      auto each = [&](auto what) {
+#pragma unroll
+        for (int k = 0; k < kElems; ++k) {
+          int c, r;
+          place(k, c, r);
+          const int col = b * kThinBlock + c;
+          if (r < small && col < large) what(k, tile[c * (SP + 1) + r], z.tall ? (size_t)col * z.cols + r : (size_t)r * z.cols + col);
         }
-      }
-      if constexpr (UPDATE) {  // (a thread reads back what it wrote itself)
+      };
+      if constexpr (UPDATE) {
+        float w[kElems];
+        each([&](int k, float, size_t at) { w[k] = u.master[matrix * elems + at]; });
+        each([&](int k, float v, size_t at) {
+          w[k] = fmaf(u.keep, w[k], -u.rate * v);
+          u.master_out[matrix * elems + at] = w[k];
+        });
         for (int s0 = 0; s0 < u.slots; s0 += 64) {
           const int s = s0 + lane;
           unsigned long long set = __ballot(s < u.slots && u.slot_expert[s < u.slots ? s : 0] == (int)matrix);
           for (; set != 0; set &= set - 1) {
             Elem* const to = (Elem*)u.slot_weights + (size_t)(s0 + __ffsll((long long)set) - 1) * elems;
-            for (int i = tid; i < kThinBlock * SP; i += 256) {
-              const int c = z.tall ? i / SP : i % kThinBlock, r = z.tall ? i % SP : i / kThinBlock, col = b * kThinBlock + c;
-              if (r < small && col < large) store_elem<Elem>(to + (z.tall ? (size_t)col * z.cols + r : (size_t)r * z.cols + col), tile[c * (SP + 1) + r]);
-            }
+            each([&](int k, float, size_t at) { store_elem<Elem>(to + at, w[k]); });
           }
         }
+      } else {
+        each([&](int, float v, size_t at) { store_elem<Elem>(out + matrix * elems + at, v); });
       }
     } else {
 #pragma unroll
       for (int q = 0; q < PLANES; ++q)
-        for (int i = tid; i < kThinBlock * SP / 8; i += 256)
+#pragma unroll
+        for (int k = 0; k < kParts8; ++k) {
+          const int i = tid + kThreads * k;
           *(u32x4_t*)(a.to + q * plane + base + (size_t)b * kThinBlock * SP + i * 8) =
               *(const u32x4_t*)(lds_x + q * L::kX + i / (SP / 8) * kPitch + i % (SP / 8) * 16);
+        }
       // G of the block: both factors are the block's rows, k (its columns) major: transposing reads
       const int k_row = 8 * quad + (in >> 2);
       auto rows = [&](int q, int i, int ks) {
@@ -269,8 +312,8 @@ __global__ __launch_bounds__(256) void thin_step_kernel(ThinArgs a, Source sourc
         return __builtin_bit_cast(f16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
       };
 #pragma unroll
-      for (int t = 0; t < NB * NB / 4; ++t) {
-        const int block = wave * (NB * NB / 4) + t, bi = block / NB, bj = block % NB;
+      for (int t = 0; t < kGram; ++t) {
+        const int block = wave * kGram + t, bi = block / NB, bj = block % NB;
         f32x4 sum = {0.f, 0.f, 0.f, 0.f};
         if constexpr (PLANES == 1) sum = gram[t];
 #pragma unroll
@@ -290,8 +333,8 @@ __global__ __launch_bounds__(256) void thin_step_kernel(ThinArgs a, Source sourc
   if constexpr (MODE != THIN_LAST) {
     float* const part = a.part_out + (matrix * a.parts + blockIdx.x) * (SP * SP);
 #pragma unroll
-    for (int t = 0; t < NB * NB / 4; ++t) {
-      const int block = wave * (NB * NB / 4) + t, bi = block / NB, bj = block % NB;
+    for (int t = 0; t < kGram; ++t) {
+      const int block = wave * kGram + t, bi = block / NB, bj = block % NB;
       *(f32x4*)(part + (16 * bi + in) * SP + 16 * bj + 4 * quad) = gram[t];
     }
   }
@@ -326,7 +369,7 @@ int32_t launch_thin(const ThinArgs& a, const Source& source, const OrthoSize& z,
   constexpr int kLds = ThinLds<SP, PLANES>::bytes;
   const int32_t rc = thin_lds<kern>(kLds);
   if (rc != LZ_OK) return rc;
-  hipLaunchKernelGGL(kern, dim3(a.parts, z.n), dim3(256), kLds, st, a, source, z, (Elem*)out, u);
+  hipLaunchKernelGGL(kern, dim3(a.parts, z.n), dim3(kThinThreads<SP>), kLds, st, a, source, z, (Elem*)out, u);
   return lz::launch_status();
 }
 
