@@ -60,9 +60,9 @@ struct AdapterWorkspace {
   void *tiles, *tiles_split;          // row tiles of the adapters' rows
   void *all_tiles, *all_tiles_split;  // of all rows as one slot
   void *xs, *dys;    // x, dy by rows
-  float* low;        // [T, rank] before the scale; bf16 kernels: of every split
-  void* dh;          // [T, rank]
-  float* sum;        // [T, max(d_in, d_out)]
+  float* low;        // [splits, T, rank]: bf16 kernels, before the scale
+  void *dh, *hs;     // [T, rank]
+  float* sum;        // [T, max(d_in, d_out)]: bf16 results before they are rounded
   // shapes on the bf16 kernels
   AdapterLists lists;
   int32_t *unit_first, *unit_adapter;
@@ -98,6 +98,7 @@ AdapterWorkspace carve(void* ws, const lz_adapter_shape* s) {
     w.low = (float*)take(4 * T * s->rank * (whole_pieces(s) ? (in > out ? in : out) : 1));
   }
   w.dh = take(eb * T * s->rank);
+  if (whole_pieces(s)) w.hs = take(eb * T * s->rank);
   w.sum = (float*)take(4 * T * d);
   if (whole_pieces(s)) {
     const size_t blocks = (T + 255) / 256, units = factor_units(s);
@@ -222,19 +223,20 @@ __global__ __launch_bounds__(64) void place_ids_kernel(const int32_t* __restrict
   }
 }
 
-// to[r] = from[map[r]], rounded to To; rows of `cols`
-template <typename From, typename To>
-__global__ __launch_bounds__(256) void move_rows_kernel(const From* __restrict__ from, const int32_t* __restrict__ map, long long rows, int cols,
-                                                        To* __restrict__ to) {
+// to[r] = from[order[r]] of two matrices (blockIdx.y).
+template <typename Elem>
+struct MoveRows {
+  const Elem* from[2];
+  Elem* to[2];
+  int cols[2];
+};
+template <typename Elem>
+__global__ __launch_bounds__(256) void move_rows_kernel(MoveRows<Elem> m, const int32_t* __restrict__ order, long long rows) {
+  const int which = blockIdx.y, cols = m.cols[which];
   for (long long r = blockIdx.x; r < rows; r += gridDim.x) {
-    const From* const src = from + (size_t)map[r] * cols;
-    for (int c = threadIdx.x; c < cols; c += 256) store_elem<To>(to + (size_t)r * cols + c, load_elem<From>(src + c));
+    const Elem* const src = m.from[which] + (size_t)order[r] * cols;
+    for (int c = threadIdx.x; c < cols; c += 256) m.to[which][(size_t)r * cols + c] = src[c];
   }
-}
-template <typename From, typename To>
-int32_t move_rows(const From* from, const int32_t* map, long long rows, int cols, To* to, hipStream_t st) {
-  hipLaunchKernelGGL((move_rows_kernel<From, To>), dim3((unsigned)(rows < 65536 ? rows : 65536)), dim3(256), 0, st, from, map, rows, cols, to);
-  return lz::launch_status();
 }
 
 template <typename Elem>
@@ -242,15 +244,13 @@ __global__ __launch_bounds__(256) void clear_kernel(Elem* __restrict__ p, size_t
   for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) p[i] = Elem(0);
 }
 
-// h[r] = scale of the row's adapter times low[r], rounded once; zero for rows without one
 template <typename Elem>
-__global__ __launch_bounds__(256) void scale_rows_kernel(const float* __restrict__ low, const float* __restrict__ scale,
-                                                         const int32_t* __restrict__ order, const int32_t* __restrict__ ids, long long T, int rank,
-                                                         Elem* __restrict__ h) {
-  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < T * rank; i += (long long)gridDim.x * 256) {
-    const int id = ids[order[i / rank]];
-    store_elem<Elem>(h + i, id >= 0 ? scale[id] * low[i] : 0.f);
-  }
+void move_rows(const MoveRows<Elem>& m, int matrices, const int32_t* order, long long rows, hipStream_t st) {
+  hipLaunchKernelGGL(move_rows_kernel<Elem>, dim3((unsigned)(rows < 32768 ? rows : 32768), matrices), dim3(256), 0, st, m, order, rows);
+}
+
+__global__ __launch_bounds__(256) void round_kernel(const float* __restrict__ from, size_t n, uint16_t* __restrict__ to) {
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) to[i] = lz::f32_to_bf16(from[i]);
 }
 
 inline unsigned blocks_of(size_t n) {
@@ -258,68 +258,183 @@ inline unsigned blocks_of(size_t n) {
   return (unsigned)(b < 4096 ? (b > 0 ? b : 1) : 4096);
 }
 
-// out (fp32) = A W, or added to it, over all rows or the adapters'
-template <typename Elem, bool WKM>
-int32_t product(const AdapterWorkspace& w, const lz_adapter_shape* s, bool by_adapter, const void* A, int K, const void* W, int n_out,
-                float* out, bool add, hipStream_t st) {
+// ---- tensors of every size and alignment, on the fp32 matrix-core kernels.  The rows of h are those of the order by adapter; shapes on
+// the bf16 kernels, one of whose calls brings unaligned tensors, keep the tokens' order of those, and h by rows in w.hs.
+
+F32Args product(const AdapterWorkspace& w, const lz_adapter_shape* s, bool by_adapter, const void* A, int K, const void* W, bool k_major, int n_out) {
   F32Args a{};
   a.A = A;
   a.W = W;
-  a.C = out;
-  a.Cacc = out;
   a.K = a.lda = K;
-  a.ldw = WKM ? n_out : K;
+  a.ldw = k_major ? n_out : K;
   a.ldc = a.n_out = n_out;
   const int S = by_adapter ? s->n : 1;
   a.w_slot = by_adapter ? (long long)K * n_out : 0;
   a.t = carve_tiles(by_adapter ? w.tiles : w.all_tiles, s->T, S, kF32Rows);
   a.t_split = carve_tiles(by_adapter ? w.tiles_split : w.all_tiles_split, s->T, S, kSplitRows);
-  if constexpr (sizeof(Elem) == 4) {
-    if (!add) return launch_f32_rows<Elem, EPI_NONE, WKM>(a, S, s->T, st);
-  } else if (!add) {  // bf16 results would be rounded here
-    const size_t n = (size_t)s->T * n_out;
-    hipLaunchKernelGGL(clear_kernel<float>, dim3(blocks_of(n)), dim3(256), 0, st, out, n);
-  }
-  return launch_f32_rows<Elem, EPI_ACCUM, WKM>(a, S, s->T, st);
+  return a;
 }
 
-// The low-rank part of either direction: h = scale (rows A^T), rounded
+// h = scale (x A^T), x by rows or, given the order, by tokens
 template <typename Elem>
-int32_t low_rank(const AdapterWorkspace& w, const lz_adapter_shape* s, const void* rows, int d, const void* A, const float* scale, void* h,
-                 hipStream_t st) {
-  const size_t n = (size_t)s->T * s->rank;
-  hipLaunchKernelGGL(clear_kernel<float>, dim3(blocks_of(n)), dim3(256), 0, st, w.low, n);  // rows without an adapter too
-  const int32_t rc = product<Elem, false>(w, s, true, rows, d, A, s->rank, w.low, true, st);
-  if (rc != LZ_OK) return rc;
-  hipLaunchKernelGGL((scale_rows_kernel<Elem>), dim3(blocks_of(n)), dim3(256), 0, st, w.low, scale, w.order, w.ids, (long long)s->T, s->rank,
-                     (Elem*)h);
+int32_t low_rank(const AdapterWorkspace& w, const lz_adapter_shape* s, const void* x, const int32_t* order, int d, const void* A, const float* scale,
+                 void* h, hipStream_t st) {
+  F32Args a = product(w, s, true, x, d, A, false, s->rank);
+  a.C = h;
+  a.slot_scale = scale;
+  a.gather = order;
+  a.gather_k = 1;
+  a.gather_T = order ? s->T : 0;
+  return launch_f32_rows<Elem, EPI_SCALED, false>(a, s->n, s->T, st);
+}
+
+// out = A W + what the adapters add to it, h B.  bf16 results are summed in w.sum and rounded once.
+template <typename Elem, bool K_MAJOR>
+int32_t projected(const AdapterWorkspace& w, const lz_adapter_shape* s, const void* A, int K, const void* W, int n_out, const void* h, const void* B,
+                  void* out, hipStream_t st) {
+  constexpr bool kFloat = sizeof(Elem) == 4;
+  const size_t elems = (size_t)s->T * n_out;
+  F32Args base = product(w, s, false, A, K, W, K_MAJOR, n_out), add = product(w, s, true, h, s->rank, B, true, n_out);
+  add.Cacc = kFloat ? (float*)out : w.sum;
+  add.row_map = w.order;
+  int32_t rc;
+  if constexpr (kFloat) {
+    base.C = out;
+    rc = launch_f32_rows<Elem, EPI_NONE, K_MAJOR>(base, 1, s->T, st);
+  } else {
+    base.Cacc = w.sum;
+    hipLaunchKernelGGL(clear_kernel<float>, dim3(blocks_of(elems)), dim3(256), 0, st, w.sum, elems);
+    rc = launch_f32_rows<Elem, EPI_ACCUM, K_MAJOR>(base, 1, s->T, st);
+  }
+  if (rc == LZ_OK) rc = launch_f32_rows<Elem, EPI_ADD_ROWS, true>(add, s->n, s->T, st);
+  if (rc != LZ_OK || kFloat) return rc;
+  hipLaunchKernelGGL(round_kernel, dim3(blocks_of(elems)), dim3(256), 0, st, w.sum, elems, (uint16_t*)out);
   return lz::launch_status();
 }
 
 template <typename Elem>
 int32_t forward(const AdapterWorkspace& w, const lz_adapter_shape* s, const void* x, const void* W, const void* a, const void* b,
                 const float* scale, void* h, void* y, hipStream_t st) {
-  int32_t rc = move_rows<Elem, Elem>((const Elem*)x, w.order, s->T, s->d_in, (Elem*)w.xs, st);
-  if (rc == LZ_OK) rc = low_rank<Elem>(w, s, w.xs, s->d_in, a, scale, h, st);
-  if (rc == LZ_OK) rc = product<Elem, true>(w, s, false, w.xs, s->d_in, W, s->d_out, w.sum, false, st);
-  if (rc == LZ_OK) rc = product<Elem, true>(w, s, true, h, s->rank, b, s->d_out, w.sum, true, st);
-  if (rc == LZ_OK) rc = move_rows<float, Elem>(w.sum, w.row_of, s->T, s->d_out, (Elem*)y, st);
-  return rc;
+  void* const by_row = whole_pieces(s) ? w.hs : h;
+  const int32_t rc = low_rank<Elem>(w, s, x, w.order, s->d_in, a, scale, by_row, st);
+  if (rc != LZ_OK) return rc;
+  if (by_row != h) move_rows(MoveRows<Elem>{{(const Elem*)by_row}, {(Elem*)h}, {s->rank}}, 1, w.row_of, s->T, st);
+  return projected<Elem, true>(w, s, x, s->d_in, W, s->d_out, by_row, b, y, st);
 }
 
 template <typename Elem>
 int32_t backward(const AdapterWorkspace& w, const lz_adapter_shape* s, const void* dy, const void* x, const void* h, const void* W,
                  const void* a, const void* b, const float* scale, void* dx, void* da, void* db, hipStream_t st) {
-  int32_t rc = move_rows<Elem, Elem>((const Elem*)x, w.order, s->T, s->d_in, (Elem*)w.xs, st);
-  if (rc == LZ_OK) rc = move_rows<Elem, Elem>((const Elem*)dy, w.order, s->T, s->d_out, (Elem*)w.dys, st);
-  if (rc == LZ_OK) rc = low_rank<Elem>(w, s, w.dys, s->d_out, b, scale, w.dh, st);
-  if (rc == LZ_OK) rc = product<Elem, false>(w, s, false, w.dys, s->d_out, W, s->d_in, w.sum, false, st);
-  if (rc == LZ_OK) rc = product<Elem, true>(w, s, true, w.dh, s->rank, a, s->d_in, w.sum, true, st);
-  if (rc == LZ_OK) rc = move_rows<float, Elem>(w.sum, w.row_of, s->T, s->d_in, (Elem*)dx, st);
-  if (rc == LZ_OK) rc = launch_f32_wgrad<Elem, EPI_NONE>(f32_wgrad<Elem>(w.dh, s->rank, w.xs, s->d_in, w.first, s->n, s->T, da, nullptr), st);
-  if (rc == LZ_OK) rc = launch_f32_wgrad<Elem, EPI_NONE>(f32_wgrad<Elem>(h, s->rank, w.dys, s->d_out, w.first, s->n, s->T, db, nullptr), st);
-  return rc;
+  const MoveRows<Elem> both{{(const Elem*)x, (const Elem*)dy}, {(Elem*)w.xs, (Elem*)w.dys}, {s->d_in, s->d_out}};
+  move_rows(both, 2, w.order, s->T, st);
+  if (whole_pieces(s)) {
+    move_rows(MoveRows<Elem>{{(const Elem*)h}, {(Elem*)w.hs}, {s->rank}}, 1, w.order, s->T, st);
+    h = w.hs;
+  }
+  int32_t rc = lz::launch_status();
+  if (rc == LZ_OK) rc = low_rank<Elem>(w, s, w.dys, nullptr, s->d_out, b, scale, w.dh, st);
+  if (rc == LZ_OK) rc = projected<Elem, false>(w, s, dy, s->d_out, W, s->d_in, w.dh, a, dx, st);
+  if (rc != LZ_OK) return rc;
+  return launch_f32_wgrads<Elem, EPI_NONE>(f32_wgrad<Elem>(w.dh, s->rank, w.xs, s->d_in, w.first, s->n, s->T, da, nullptr),
+                                           f32_wgrad<Elem>(h, s->rank, w.dys, s->d_out, w.first, s->n, s->T, db, nullptr), true, st);
 }
+
+// Few tokens: the sort and the tables in one launch, where the steps above and the tables' own kernel are five of 3 to 6 us each.  A
+// wave has a run of the tokens, whose counts lie in LDS, one after the other for every adapter.
+constexpr int kSmallTokens = 4096, kSmallAdapters = 1000;
+struct SmallPlan {
+  const int32_t* ids;
+  int32_t *clean, *first, *order, *row_of, *all, *status;
+  TileTable tiles, tiles_split, all_tiles, all_tiles_split;
+  int T, n;
+};
+__global__ __launch_bounds__(1024) void small_plan_kernel(SmallPlan p) {
+  extern __shared__ int32_t counts[];  // [16][n + 1]
+  __shared__ int32_t waves[3][16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, T = p.T, n = p.n;
+  const int run = (T + 1023) / 1024 * 64, t0 = wave * run;
+  for (int i = tid; i < 16 * (n + 1); i += 1024) counts[i] = 0;
+  __syncthreads();
+  bool bad = false;
+  for (int t = t0 + lane; t < t0 + run && t < T; t += 64) {
+    int id = p.ids[t];
+    bad |= id < -1 || id >= n;
+    id = id >= 0 && id < n ? id : -1;
+    p.clean[t] = id;
+    atomicAdd(&counts[wave * (n + 1) + (id < 0 ? n : id)], 1);
+  }
+  const int any = __syncthreads_or(bad);
+  if (tid == 0 && p.status != nullptr) *p.status = any ? LZ_ADAPTER_BAD_ID : 0;
+  int total = 0;
+  for (int w = 0; tid <= n && w < 16; ++w) {
+    int32_t& at = counts[w * (n + 1) + tid];
+    const int here = at;
+    at = total;
+    total += here;
+  }
+  // first row of the thread's adapter, and its first tiles
+  auto add = [](int x, int y) { return x + y; };
+  const int own[3] = {total, tid < n ? (total + kF32Rows - 1) / kF32Rows : 0, tid < n ? (total + kSplitRows - 1) / kSplitRows : 0};
+  int incl[3];
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    incl[i] = lz::wave_scan(own[i], add);
+    if (lane == 63) waves[i][wave] = incl[i];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    incl[i] -= own[i];
+    for (int w = 0; w < wave; ++w) incl[i] += waves[i][w];
+  }
+  const int row0 = incl[0];
+  if (tid <= n) {
+    p.first[tid] = row0;
+    for (int w = 0; w < 16; ++w) counts[w * (n + 1) + tid] += row0;
+  }
+  if (tid == 0) {
+    p.first[n + 1] = T;
+    p.all[0] = 0;
+    p.all[1] = T;
+  }
+  auto entry = [&](const TileTable& t, int i, int slot, int from, int end) {
+    t.slot[i] = slot;
+    t.row0[i] = from;
+    t.row_end[i] = end;
+  };
+  for (int i = 0; i < own[1]; ++i) entry(p.tiles, incl[1] + i, tid, row0 + i * kF32Rows, row0 + total);
+  for (int i = 0; i < own[2]; ++i) entry(p.tiles_split, incl[2] + i, tid, row0 + i * kSplitRows, row0 + total);
+  if (tid == n) {
+    p.tiles.header[0] = incl[1];
+    p.tiles_split.header[0] = incl[2];
+    p.all_tiles.header[0] = (T + kF32Rows - 1) / kF32Rows;
+    p.all_tiles_split.header[0] = (T + kSplitRows - 1) / kSplitRows;
+  }
+  if (tid * kF32Rows < T) entry(p.all_tiles, tid, 0, tid * kF32Rows, T);
+  if (tid * kSplitRows < T) entry(p.all_tiles_split, tid, 0, tid * kSplitRows, T);
+  __syncthreads();
+  int32_t* const next = counts + wave * (n + 1);
+  for (int t1 = t0; t1 < t0 + run && t1 < T; t1 += 64) {
+    const int t = t1 + lane;
+    int id = t < T ? p.clean[t] : -2;
+    if (id == -1) id = n;
+    for (unsigned long long left = __ballot(id >= 0); left != 0;) {
+      const int leader = __ffsll((long long)left) - 1, a = __shfl(id, leader);
+      const unsigned long long same = __ballot(id == a);
+      const int base = next[a];
+      if (id == a) {
+        const int row = base + __popcll(same & ((1ull << lane) - 1));
+        p.order[row] = t;
+        p.row_of[t] = row;
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // (the wave's own counts)
+      if (lane == leader) next[a] = base + __popcll(same);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      left &= ~same;
+    }
+  }
+}
+static_assert(kSmallTokens / kF32Rows <= 1024, "a thread per tile of all rows");
 
 // Tokens by adapter: w.order, w.row_of, w.first, and what the shape's kernels take their work from.
 int32_t sort_tokens(const AdapterWorkspace& w, const lz_adapter_shape* s, hipStream_t st, int32_t* status = nullptr, const int32_t* ids = nullptr) {
@@ -334,6 +449,13 @@ int32_t sort_tokens(const AdapterWorkspace& w, const lz_adapter_shape* s, hipStr
 // ... for the kernels of every size
 int32_t sort_with_tables(const AdapterWorkspace& w, const lz_adapter_shape* s, hipStream_t st, int32_t* status = nullptr,
                          const int32_t* ids = nullptr) {
+  if (s->T <= kSmallTokens && s->n <= kSmallAdapters) {
+    const SmallPlan p{ids ? ids : w.ids, w.ids, w.first, w.order, w.row_of, w.all, status, carve_tiles(w.tiles, s->T, s->n, kF32Rows),
+                      carve_tiles(w.tiles_split, s->T, s->n, kSplitRows), carve_tiles(w.all_tiles, s->T, 1, kF32Rows),
+                      carve_tiles(w.all_tiles_split, s->T, 1, kSplitRows), s->T, s->n};
+    hipLaunchKernelGGL(small_plan_kernel, dim3(1), dim3(1024), 4 * 16 * (size_t)(s->n + 1), st, p);
+    return lz::launch_status();
+  }
   int32_t rc = sort_tokens(w, s, st, status, ids);
   if (rc != LZ_OK) return rc;
   auto tables = [&](const int32_t* offsets, int S, void* rows, void* split) {
@@ -445,9 +567,9 @@ extern "C" int32_t lz_adapter_plan(const int32_t* ids, const lz_adapter_shape* s
   if (rc != LZ_OK) return rc;
   hipStream_t st = (hipStream_t)stream;
   if (shape->T > 0 && !ids) return LZ_EINVAL;
-  // (one workgroup of the lists' kernel writes the word by itself)
-  if (status_opt && !(whole_pieces(shape) && shape->T > 0 && shape->T <= 256))
-    hipLaunchKernelGGL(clear_status_kernel, dim3(1), dim3(1), 0, st, status_opt);
+  // (kernels of one workgroup write the word by themselves)
+  const bool alone = whole_pieces(shape) ? shape->T <= 256 : shape->T <= kSmallTokens && shape->n <= kSmallAdapters;
+  if (status_opt && (shape->T == 0 || !alone)) hipLaunchKernelGGL(clear_status_kernel, dim3(1), dim3(1), 0, st, status_opt);
   if (shape->T == 0) return lz::launch_status();
   if (!whole_pieces(shape)) return sort_with_tables(w, shape, st, status_opt, ids);
   hipLaunchKernelGGL(adapter_lists_kernel, dim3(ceil_div(shape->T, 256)), dim3(256), 4 * (size_t)shape->n, st, ids, shape->T, shape->n, w.ids,

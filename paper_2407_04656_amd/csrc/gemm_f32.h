@@ -23,7 +23,8 @@
 namespace {
 
 // dZ = dH * act'(Z) in the epilogue of dH = dyp W2^T: C is dZ, Z is read
-enum { EPI_DGELU = 6, EPI_DSWIGLU = 7 };
+// EPI_SCALED: C = slot_scale[slot] times the sum.  EPI_ADD_ROWS: the sum is added to row row_map[row] of Cacc.
+enum { EPI_DGELU = 6, EPI_DSWIGLU = 7, EPI_SCALED = 15, EPI_ADD_ROWS = 16 };
 
 constexpr int kF32Rows = 32;  // rows of a tile
 
@@ -47,6 +48,8 @@ struct F32Args {
   const int32_t* slot_offsets;  // weight gradients
   long long P;
   int m_rows;           // weight gradients: rows of one slot's result
+  const float* slot_scale;  // EPI_SCALED
+  const int32_t* row_map;   // EPI_ADD_ROWS
 };
 
 template <typename Elem>
@@ -115,6 +118,11 @@ __device__ __forceinline__ void f32_emit(const F32Args& a, int slot, int row, in
   const int n = row < row_end ? a.n_out - col : 0;
   const size_t grow = WGRAD ? (size_t)slot * a.m_rows + row : (size_t)row;
   if (n <= 0) return;
+  if constexpr (EPI == EPI_ADD_ROWS) {
+    float* const s = a.Cacc + (size_t)a.row_map[row] * a.ldc + col;
+    store_piece<float, VEC>(s, load_piece<float, VEC>(s, a.Cacc, n) + v, n);
+    return;
+  }
   Elem* const c = (Elem*)a.C + grow * a.ldc + col;
   if constexpr (EPI == EPI_ACCUM) {
     float* const s = a.Cacc + grow * a.ldc + col;
@@ -127,6 +135,7 @@ __device__ __forceinline__ void f32_emit(const F32Args& a, int slot, int row, in
     if constexpr (kGated) store_piece<Elem, VEC>(z + a.ffn, u, n);
   }
   f32x4 o = v, o2;
+  if constexpr (EPI == EPI_SCALED) o = a.slot_scale[slot] * v;
   if constexpr (EPI == EPI_DGELU || EPI == EPI_DSWIGLU) {
     const Elem* const z = (const Elem*)a.Z + grow * a.ldz + col;
     const f32x4 zg = load_piece<Elem, VEC>(z, (const Elem*)a.Z, n);

@@ -32,6 +32,8 @@ ODD = [  # sizes that only single elements fit
     (5, 3, 7, 2, 2, 3, 0.3),
     (129, 77, 131, 5, 4, 9, 0.2),
     (1021, 100, 261, 12, 9, 9, 0.2),
+    (4200, 33, 20, 3, 50, 700, 0.1),
+    (300, 20, 36, 4, 1500, 300, 0.1),
 ]
 
 
@@ -134,6 +136,29 @@ def test_tensors_off_16_byte_alignment(dtype):
     y = p.forward(off(s["x"]))
     grads = p.backward(off(s["dy"]))
     ref = reference(s, dtype)
+    for name, got in zip(("y", "dx", "da", "db"), (y, *grads)):
+        check(name, got, *ref[name])
+
+
+@pytest.mark.parametrize("forward_off", [False, True])
+def test_forward_and_backward_of_different_alignment(forward_off):
+    """What the forward keeps is the backward's whichever kernels their tensors' alignment leads to."""
+    T, d_in, d_out, rank, n = 200, 128, 192, 16, 5
+    s = inputs(T, d_in, d_out, rank, n, BF16, tokens(np.random.default_rng(3), T, n, 9, 0.2), 3)
+
+    def off(t):
+        room = torch.empty(t.numel() + 1, dtype=t.dtype, device=DEV)
+        view = room[1:].view(t.shape)
+        view.copy_(t)
+        return view
+
+    p = projection(s, T, d_in, d_out, rank, n, BF16)
+    p.plan(s["ids"].to(DEV))
+    x, dy = s["x"].to(DEV), s["dy"].to(DEV)
+    y = p.forward(off(x) if forward_off else x).clone()
+    p.x = x
+    grads = p.backward(dy if forward_off else off(dy))
+    ref = reference(s, BF16)
     for name, got in zip(("y", "dx", "da", "db"), (y, *grads)):
         check(name, got, *ref[name])
 
