@@ -506,12 +506,12 @@ int32_t projection(const AdapterWorkspace& w, const lz_adapter_shape* s, const v
   a.W = (const uint16_t*)W;
   a.C = (uint16_t*)out;
   a.P = s->T;
-  a.matrices = 1;
   a.rows_each = s->T;
   a.K = K;
   a.w_rows = n_out;
   a.n_out = a.ldw = n_out;
   a.n_tiles = ceil_div(n_out, BN);
+  a.fixed = ceil_div(s->T, BM) * a.n_tiles;
   a.adapter = AdapterSteps{(const uint16_t*)h, (const uint16_t*)b, w.lists.count256, w.lists.list256, w.lists.local256, s->rank};
   return launch_mfma<EPI_ADAPTER, MODE>(a, st);
 }

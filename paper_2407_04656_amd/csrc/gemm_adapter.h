@@ -11,19 +11,6 @@
 
 namespace {
 
-// Lets a kernel have so much dynamic LDS; once per device (idempotent).
-template <auto KERNEL>
-int32_t allow_lds(int bytes) {
-  static std::atomic<bool> ready_on_device[kMaxDevices];
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return LZ_EHIP;
-  if (!ready_on_device[dev].load(std::memory_order_acquire)) {
-    if (hipFuncSetAttribute((const void*)KERNEL, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return LZ_EHIP;
-    ready_on_device[dev].store(true, std::memory_order_release);
-  }
-  return LZ_OK;
-}
-
 // Which adapters the tokens of 256 and of 64 consecutive rows use, and where in that list each row's stands (255: none).
 struct AdapterLists {
   int32_t *count256, *list256;

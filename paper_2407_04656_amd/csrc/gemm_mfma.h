@@ -108,7 +108,8 @@ struct MfmaArgs {
   long long gather_T;
   AdapterSteps adapter;
   // EPI_ADAPTER, kOrtho: equal matrices of so many rows each
-  int matrices, rows_each;
+  int rows_each;
+  int fixed;  // tiles of the launch
   OrthoProduct ortho;
 };
 
@@ -701,18 +702,46 @@ struct Draws {
 
 // Tiles that cost the same, of equal matrices: no queue, no table.  Each XCD has a run of the tiles, in bands of kGroupM row tiles,
 // the columns of a band one after the other: what an XCD works on at a time are kGroupM x 8 tiles that share panels.
+struct FixedTile {
+  int matrix, row, col;
+};
+// SYMMETRIC: tiles on and below the diagonal alone.
+template <bool SYMMETRIC>
+__host__ __device__ __forceinline__ int fixed_tiles(int m_tiles, int n_tiles) { return SYMMETRIC ? m_tiles * (m_tiles + 1) / 2 : m_tiles * n_tiles; }
+template <bool SYMMETRIC>
+__device__ __forceinline__ FixedTile fixed_tile(int index, int m_tiles, int n_tiles) {
+  const int each = fixed_tiles<SYMMETRIC>(m_tiles, n_tiles), matrix = index / each, t = index - matrix * each;
+  int row, col;
+  if constexpr (SYMMETRIC) {  // 8 b^2 + 2 b tiles lie above band b
+    int b = 0;
+    while (8 * (b + 1) * (b + 1) + 2 * (b + 1) <= t) ++b;
+    const int left = m_tiles - b * kGroupM, nr = left < kGroupM ? left : kGroupM, within = t - (8 * b * b + 2 * b);
+    if (within < kGroupM * b * nr) {
+      col = within / nr;
+      row = b * kGroupM + within - col * nr;
+    } else {  // the band's triangle
+      int w = within - kGroupM * b * nr, j = 0;
+      for (; w >= nr - j; ++j) w -= nr - j;
+      col = b * kGroupM + j;
+      row = col + w;
+    }
+  } else {
+    const int band = t / (kGroupM * n_tiles), within = t - band * kGroupM * n_tiles;
+    const int left = m_tiles - band * kGroupM, nr = left < kGroupM ? left : kGroupM;
+    col = within / nr;
+    row = band * kGroupM + within - col * nr;
+  }
+  // (divided by the vector unit: back to scalar registers, where descriptors are made)
+  return FixedTile{__builtin_amdgcn_readfirstlane(matrix), __builtin_amdgcn_readfirstlane(row), __builtin_amdgcn_readfirstlane(col)};
+}
 template <bool SYMMETRIC>
 struct FixedDraws {
   const MfmaArgs& a;
-  int at, end;             // this workgroup's tile, the XCD's last
-  int m_tiles, each;       // row tiles and tiles of a matrix
+  int at, end;  // this workgroup's tile, the XCD's last
   __device__ __forceinline__ FixedDraws(const MfmaArgs& args, char*) : a(args) {
     const int xcd = blockIdx.x % 8;
-    m_tiles = (a.rows_each + BM - 1) / BM;
-    each = SYMMETRIC ? m_tiles * (m_tiles + 1) / 2 : m_tiles * a.n_tiles;
-    const long long tiles = (long long)a.matrices * each;
-    at = int(tiles * xcd / 8) + (int)(blockIdx.x / 8);
-    end = int(tiles * (xcd + 1) / 8);
+    at = int((long long)a.fixed * xcd / 8) + (int)(blockIdx.x / 8);
+    end = int((long long)a.fixed * (xcd + 1) / 8);
   }
   __device__ __forceinline__ void request() {}
   __device__ __forceinline__ void publish(char*) {}
@@ -723,31 +752,9 @@ struct FixedDraws {
   __device__ __forceinline__ void finish() {}
   __device__ __forceinline__ Tile tile(int n_out_cols) const {
     if (at >= end) return Tile{-1, 0, 0, 0, 0, 0, 0};
-    const int matrix = at / each, t = at - matrix * each;
-    int row, col;
-    if constexpr (SYMMETRIC) {  // rows of a band: 8 b^2 + 2 b tiles lie above band b
-      int b = 0;
-      while (8 * (b + 1) * (b + 1) + 2 * (b + 1) <= t) ++b;
-      const int left = m_tiles - b * kGroupM, nr = left < kGroupM ? left : kGroupM, within = t - (8 * b * b + 2 * b);
-      if (within < kGroupM * b * nr) {
-        col = within / nr;
-        row = b * kGroupM + within - col * nr;
-      } else {  // the band's triangle
-        int w = within - kGroupM * b * nr, j = 0;
-        for (; w >= nr - j; ++j) w -= nr - j;
-        col = b * kGroupM + j;
-        row = col + w;
-      }
-    } else {
-      const int band = t / (kGroupM * a.n_tiles), within = t - band * kGroupM * a.n_tiles;
-      const int left = m_tiles - band * kGroupM, nr = left < kGroupM ? left : kGroupM;
-      col = within / nr;
-      row = band * kGroupM + within - col * nr;
-    }
-    // (divided by the vector unit: back to scalar registers, where descriptors are made)
-    auto scalar = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
-    const int slot = scalar(matrix), row0 = scalar(slot * a.rows_each + row * BM), row_end = (slot + 1) * a.rows_each;
-    return Tile{slot, row0, row_end - row0 < BM ? row_end : row0 + BM, scalar(col * n_out_cols), 0, 0, 0};
+    const FixedTile t = fixed_tile<SYMMETRIC>(at, (a.rows_each + BM - 1) / BM, a.n_tiles);
+    const int row0 = t.matrix * a.rows_each + t.row * BM, row_end = (t.matrix + 1) * a.rows_each;
+    return Tile{t.matrix, row0, row_end - row0 < BM ? row_end : row0 + BM, t.col * n_out_cols, 0, 0, 0};
   }
 };
 template <int EPI>

@@ -204,6 +204,19 @@ __global__ __launch_bounds__(256, 2) void gemm_narrow_kernel(MfmaArgs a) {
 #endif
 }
 
+// Lets a kernel have so much dynamic LDS; once per device (idempotent).
+template <auto KERNEL>
+int32_t allow_lds(int bytes) {
+  static std::atomic<bool> ready_on_device[kMaxDevices];
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return LZ_EHIP;
+  if (!ready_on_device[dev].load(std::memory_order_acquire)) {
+    if (hipFuncSetAttribute((const void*)KERNEL, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return LZ_EHIP;
+    ready_on_device[dev].store(true, std::memory_order_release);
+  }
+  return LZ_OK;
+}
+
 template <int EPI, int MODE, bool GATHER, bool KTAIL>
 int32_t launch_narrow_kernel(const MfmaArgs& a, hipStream_t st) {
   void (*kern)(MfmaArgs) = gemm_narrow_kernel<EPI, MODE, GATHER, KTAIL>;

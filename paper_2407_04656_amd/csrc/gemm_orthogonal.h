@@ -31,6 +31,8 @@ struct OrthoArgs {
   int n, sp, lp;
   float mu, c2, lin, diag, rho;  // diag = q0 - rho
   int pairs;                     // of planes that a product of two planes sums: 3, or 1: hi hi alone
+  int tiles = 0;                 // of the launch
+  int wide_from = -1;            // >= 0: they are those of the wide kernel's from here on, 16 each
 };
 
 __device__ __forceinline__ float f16_value(uint16_t b) { return (float)__builtin_bit_cast(_Float16, b); }
@@ -60,30 +62,54 @@ __device__ __forceinline__ void load_planes8(const uint16_t* from, size_t plane,
   }
 }
 
-// 64 x 64 tiles, four waves of 32 x 32, a ring of four K steps of 64 as in gemm_narrow.h.  GRAM and SQUARE are symmetric: only tiles
-// on and below the diagonal are computed, and stored twice.  blockIdx.x = tile, blockIdx.y = matrix.
+// 64 x 64 tiles, a ring of four K steps of 64 as in gemm_narrow.h; eight waves of 32 x 32, either four of which take half of a step's k
+// and add up through LDS at the end, a step's products while the next one's fragments are on their way.  A step takes 0.3 us, a quarter of
+// it products: 16 KB into LDS and 32 KB out of it, one after the other at a barrier.  Four waves of all k, fragments without the
+// step ahead, and a ring of eight steps were within 7 % of this.
+// GRAM and SQUARE are symmetric: only tiles
+// on and below the diagonal are computed, and stored twice.  A launch takes all tiles, or
+// what is left of a wide one's (a.wide_from).
+constexpr int kOrthoThreads = 512;
 template <int KIND, int PLANES>
-__global__ __launch_bounds__(256, 2) void ortho_narrow_kernel(OrthoArgs a) {
+__global__ __launch_bounds__(kOrthoThreads, 4) void ortho_narrow_kernel(OrthoArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr bool TB = KIND == KIND_APPLY;  // W k-major
-  constexpr int NS = kNarrowStages, kLoads = 4;
+  constexpr int NS = kNarrowStages, kLoads = 2;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int sp = a.sp, lp = a.lp;
-  int tm, tn;
-  if constexpr (TB) {
-    const int cols = lp / kNarrow;
-    tm = blockIdx.x / cols;
-    tn = blockIdx.x % cols;
-  } else {  // the row tm of the triangle with tm (tm + 1) / 2 <= tile
-    tm = (int)((__fsqrt_rn(8.f * (float)blockIdx.x + 1.f) - 1.f) * 0.5f);
-    while ((tm + 1) * (tm + 2) / 2 <= (int)blockIdx.x) ++tm;
-    while (tm * (tm + 1) / 2 > (int)blockIdx.x) --tm;
-    tn = (int)blockIdx.x - tm * (tm + 1) / 2;
+  // Workgroups are dealt to the 8 XCDs in turn: each XCD has a run of the tiles, which share panels in its L2 (dealt in turn, APPLY
+  // of five 777 x 333 matrices in two planes takes 14.8 us, so 13.3).
+  const int at_xcd = (int)((long long)a.tiles * (blockIdx.x % 8) / 8) + (int)(blockIdx.x / 8);
+  if (at_xcd >= (int)((long long)a.tiles * (blockIdx.x % 8 + 1) / 8)) return;
+  int tm, tn, matrix;
+  if (a.wide_from >= 0) {  // 16 tiles of a wide one
+    const FixedTile t = fixed_tile<!TB>(a.wide_from + at_xcd / 16, (sp + BM - 1) / BM, (lp + BN - 1) / BN);
+    matrix = t.matrix;
+    tm = t.row * 4 + at_xcd / 4 % 4;
+    tn = t.col * 4 + at_xcd % 4;
+    if (tm >= sp / kNarrow || tn >= (TB ? lp : sp) / kNarrow || (!TB && tn > tm)) return;
+  } else {
+    const int m = sp / kNarrow, each = TB ? m * (lp / kNarrow) : m * (m + 1) / 2;
+    matrix = at_xcd / each;
+    const int t = at_xcd - matrix * each;
+    if constexpr (TB) {
+      const int cols = lp / kNarrow;
+      tm = t / cols;
+      tn = t % cols;
+    } else {  // the row tm of the triangle with tm (tm + 1) / 2 <= t
+      tm = (int)((__fsqrt_rn(8.f * (float)t + 1.f) - 1.f) * 0.5f);
+      while ((tm + 1) * (tm + 2) / 2 <= t) ++tm;
+      while (tm * (tm + 1) / 2 > t) --tm;
+      tn = t - tm * (tm + 1) / 2;
+    }
+    matrix = __builtin_amdgcn_readfirstlane(matrix);
+    tm = __builtin_amdgcn_readfirstlane(tm);
+    tn = __builtin_amdgcn_readfirstlane(tn);
   }
   const int m0 = tm * kNarrow, n0 = tn * kNarrow;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = wave >> 1, wn = wave & 1;
-  const size_t large = (size_t)sp * lp, small = (size_t)sp * sp, at = blockIdx.y;
+  const int ks = wave >> 2, wm = (wave >> 1) & 1, wn = wave & 1;
+  const size_t large = (size_t)sp * lp, small = (size_t)sp * sp, at = matrix;
   const uint16_t* const matA = KIND == KIND_GRAM ? a.X + at * large : KIND == KIND_SQUARE ? a.H + at * small : a.P + at * small;
   const uint16_t* const matW = KIND == KIND_SQUARE ? a.H + at * small : a.X + at * large;
   const size_t planeA = (KIND == KIND_GRAM ? large : small) * a.n, planeW = (KIND == KIND_SQUARE ? small : large) * a.n;
@@ -91,35 +117,24 @@ __global__ __launch_bounds__(256, 2) void ortho_narrow_kernel(OrthoArgs a) {
   const uint32_t extentA = (uint32_t)((KIND == KIND_GRAM ? large : small) * 2), extentW = (uint32_t)((KIND == KIND_SQUARE ? small : large) * 2);
   const int stepW = TB ? BK * ldw * 2 : BK * 2;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
-  int voffX[2], voffW[2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int r = (wave * 2 + i) * 8 + (lane >> 3);
-    const int chunk = (lane & 7) ^ swz(r);
-    voffX[i] = (int)(((uint32_t)(m0 + r) * (uint32_t)K + (uint32_t)chunk * 8u) * 2u);
-    if constexpr (TB) voffW[i] = (int)(((uint32_t)r * (uint32_t)ldw + (uint32_t)(n0 + ((lane & 7) ^ swz_narrow(r)) * 8)) * 2u);
-    else voffW[i] = (int)(((uint32_t)(n0 + r) * (uint32_t)K + (uint32_t)chunk * 8u) * 2u);
-  }
+  const int load_row = wave * 8 + (lane >> 3), load_chunk = (lane & 7) ^ swz(load_row);
+  const int voffX = (int)(((uint32_t)(m0 + load_row) * (uint32_t)K + (uint32_t)load_chunk * 8u) * 2u);
+  const int voffW = TB ? (int)(((uint32_t)load_row * (uint32_t)ldw + (uint32_t)(n0 + ((lane & 7) ^ swz_narrow(load_row)) * 8)) * 2u)
+                       : (int)(((uint32_t)(n0 + load_row) * (uint32_t)K + (uint32_t)load_chunk * 8u) * 2u);
   const int k_steps = K / BK, all_steps = PLANES == 2 ? a.pairs * k_steps : k_steps;
   int seg = 0, k = 0;  // of the next step to load: which pair of planes, step within it
   auto issue = [&](bool real, int stage) {  // a step past the end writes zeros, without memory traffic
     const i32x4 wa = rsrc_words(matA + (seg == 2 ? planeA : 0), real ? extentA : 0), ww = rsrc_words(matW + (seg == 1 ? planeW : 0), real ? extentW : 0);
-    const uint32_t lds = lds0 + stage * kNarrowStage;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) load16_to_lds(ww, lds + kNarrowOperand + (wave * 2 + i) * 1024, voffW[i], k * stepW);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) load16_to_lds(wa, lds + (wave * 2 + i) * 1024, voffX[i], k * BK * 2);
+    const uint32_t lds = lds0 + stage * kNarrowStage + wave * 1024;
+    load16_to_lds(ww, lds + kNarrowOperand, voffW, k * stepW);
+    load16_to_lds(wa, lds, voffX, k * BK * 2);
     if (++k == k_steps) {
       k = 0;
       ++seg;
     }
   };
-  int fragoff[2], woff[2];
-#pragma unroll
-  for (int ks = 0; ks < 2; ++ks) {
-    const int r = lane & 15;
-    fragoff[ks] = r * kRowBytes + (((ks * 4 + (lane >> 4)) ^ swz(r)) << 4);
-  }
+  int woff[2];
+  const int fragoff = (lane & 15) * kRowBytes + (((ks * 4 + (lane >> 4)) ^ swz(lane & 15)) << 4);
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
     if constexpr (TB) {
@@ -129,59 +144,67 @@ __global__ __launch_bounds__(256, 2) void ortho_narrow_kernel(OrthoArgs a) {
       woff[c] = (2 * wn + c) * 16 * kRowBytes;
     }
   }
-  auto read_x = [&](const char* st, int ks, int j) { return *(const f16x8*)(st + (2 * wm + j) * 16 * kRowBytes + fragoff[ks]); };
-  auto read_w = [&](const char* st, int ks, int c) {
+  auto read_x = [&](const char* st, int j) { return *(const f16x8*)(st + (2 * wm + j) * 16 * kRowBytes + fragoff); };
+  auto read_w = [&](const char* st, int c) {
     if constexpr (TB) {
       const char* p = st + kNarrowOperand + woff[c] + ks * 32 * kRowBytes;
       const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)p);
       const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(p + 4 * kRowBytes));
       return __builtin_bit_cast(f16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     } else {
-      return *(const f16x8*)(st + kNarrowOperand + woff[c] + fragoff[ks]);
+      return *(const f16x8*)(st + kNarrowOperand + woff[c] + fragoff);
     }
   };
   f32x4 acc[2][2] = {};
 #pragma unroll
   for (int s = 0; s < NS - 1; ++s) issue(s < all_steps, s);
   int stage = 0;
+  f16x8 x[2] = {}, w[2] = {};
+  auto multiply = [&]() {
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) acc[c][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[c], x[j], acc[c][j], 0, 0, 0);
+  };
   for (int kt = 0; kt < all_steps; ++kt) {
     constexpr int kAhead = (NS - 2) * kLoads;
     __builtin_amdgcn_s_waitcnt(0x0F70 | (kAhead & 15) | ((kAhead >> 4) << 14));  // this wave's loads of step kt are in LDS
     __syncthreads();  // ... everyone's are; and nobody reads the stage of step kt - 1 any more
     issue(kt + NS - 1 < all_steps, stage == 0 ? NS - 1 : stage - 1);
     const char* const st = smem + stage * kNarrowStage;
+    f16x8 xn[2], wn_[2];
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      f16x8 x[2], w[2];
+    for (int c = 0; c < 2; ++c) wn_[c] = read_w(st, c);
 #pragma unroll
-      for (int c = 0; c < 2; ++c) w[c] = read_w(st, ks, c);
+    for (int j = 0; j < 2; ++j) xn[j] = read_x(st, j);
+    multiply();  // the step before, while this one's fragments are on their way
 #pragma unroll
-      for (int j = 0; j < 2; ++j) x[j] = read_x(st, ks, j);
-#pragma unroll
-      for (int c = 0; c < 2; ++c)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) acc[c][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[c], x[j], acc[c][j], 0, 0, 0);
-    }
+    for (int c = 0; c < 2; ++c) w[c] = wn_[c], x[c] = xn[c];
     stage = stage + 1 == NS ? 0 : stage + 1;
   }
+  multiply();
   // the trailing loads still write zeros into stages: drained by every wave before the tile overwrites them
   __builtin_amdgcn_s_waitcnt(0x0F70);
   __syncthreads();
   // the tile, fp32, [row][column] through LDS, so that both it and its mirror image leave in 16-byte pieces
   constexpr int kPitch = kNarrow + 1;
   float* const tile = (float*)smem;
+  auto each = [&](auto what) {
 #pragma unroll
-  for (int c = 0; c < 2; ++c)
+    for (int c = 0; c < 2; ++c)
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+      for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int v = 0; v < 4; ++v)
-        tile[(32 * wm + 16 * j + (lane & 15)) * kPitch + 32 * wn + 16 * c + 4 * (lane >> 4) + v] = acc[c][j][v];
+        for (int v = 0; v < 4; ++v)
+          what(tile[(32 * wm + 16 * j + (lane & 15)) * kPitch + 32 * wn + 16 * c + 4 * (lane >> 4) + v], acc[c][j][v]);
+  };
+  if (ks == 0) each([](float& to, float v) { to = v; });
+  __syncthreads();
+  if (ks == 1) each([](float& to, float v) { to += v; });
   __syncthreads();
   constexpr float kDown = 1.f / kOrthoScale;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int p = threadIdx.x + 256 * i, r = p >> 3, c = (p & 7) * 8;
+  {
+    const int r = threadIdx.x >> 3, c = (threadIdx.x & 7) * 8;
     float v[8];
     if constexpr (KIND == KIND_APPLY) {
       const size_t to = at * large + (size_t)(m0 + r) * lp + n0 + c;
@@ -229,11 +252,10 @@ bool use_wide(const OrthoArgs& a) {
   return tiles >= 96 && a.sp > BK && (KIND != KIND_SQUARE || (a.lin == 0.f && a.c2 != 0.f));
 }
 template <int KIND, int PLANES>
-int32_t launch_ortho_wide(const OrthoArgs& a, hipStream_t st) {
+int32_t launch_ortho_wide(const OrthoArgs& a, int tiles, hipStream_t st) {
   constexpr bool kTwo = PLANES == 2;
   const size_t small = (size_t)a.n * a.sp * a.sp, large = (size_t)a.n * a.sp * a.lp;
   MfmaArgs g{};
-  g.matrices = a.n;
   g.rows_each = a.sp;
   g.P = (long long)a.n * a.sp;
   if constexpr (KIND == KIND_APPLY) {
@@ -251,18 +273,39 @@ int32_t launch_ortho_wide(const OrthoArgs& a, hipStream_t st) {
     else g.ortho = OrthoProduct{from, from, small, a.c2 / kOrthoScale, a.diag / a.c2 * kOrthoScale * kOrthoScale, a.residual, 0.f, a.pairs};
   }
   g.n_tiles = ceil_div(g.n_out, BN);
+  g.fixed = tiles;
   constexpr int kEpi = KIND == KIND_GRAM ? (kTwo ? EPI_GRAM_TWO : EPI_GRAM)
                        : KIND == KIND_SQUARE ? (kTwo ? EPI_SQUARE_TWO : EPI_SQUARE) : (kTwo ? EPI_APPLY_TWO : EPI_APPLY);
   return launch_mfma_kernel<kEpi, KIND == KIND_APPLY ? MODE_NN : MODE_NT, false, false, false>(MfmaLaunch<false>{{g}}, st);
 }
 
 template <int KIND, int PLANES>
-int32_t launch_ortho(const OrthoArgs& a, hipStream_t st) {
-  if (use_wide<KIND, PLANES>(a)) return launch_ortho_wide<KIND, PLANES>(a, st);
-  const int m = a.sp / kNarrow;
-  const long long tiles = KIND == KIND_APPLY ? (long long)m * (a.lp / kNarrow) : (long long)m * (m + 1) / 2;
-  hipLaunchKernelGGL((ortho_narrow_kernel<KIND, PLANES>), dim3((unsigned)tiles, (unsigned)a.n), dim3(256), kNarrowLds, st, a);
+int32_t launch_ortho_narrow(OrthoArgs a, long long tiles, hipStream_t st) {
+  if (tiles > 0x7FFFFFF0ll) return LZ_ESHAPE;
+  a.tiles = (int)tiles;
+  const dim3 grid((unsigned)((tiles + 7) / 8 * 8)), threads(kOrthoThreads);
+  hipLaunchKernelGGL((ortho_narrow_kernel<KIND, PLANES>), grid, threads, kNarrowLds, st, a);
   return lz::launch_status();
+}
+
+// The wide tiles that a launch's last round would have, where they are few, go to the narrow kernel: 16 tiles each, of which the chip
+// holds 512 at a time.  A round costs as much for one tile as for all: two 4096 x 14336 matrices, 272 tiles, GRAM 580 us, of which the 16
+// last take half, and 436 with them apart; with 64 left of 1344 it is level.
+constexpr int kFewLeft = 48;
+template <int KIND, int PLANES>
+int32_t launch_ortho(OrthoArgs a, hipStream_t st) {
+  constexpr bool kSym = KIND != KIND_APPLY;
+  if (use_wide<KIND, PLANES>(a)) {
+    const int workgroups = device_cus(), tiles = a.n * fixed_tiles<kSym>(ceil_div(a.sp, BM), ceil_div(a.lp, BN));
+    if (workgroups == 0) return LZ_EHIP;
+    const int left = tiles > workgroups && tiles % workgroups <= kFewLeft ? tiles % workgroups : 0;
+    const int32_t rc = launch_ortho_wide<KIND, PLANES>(a, tiles - left, st);
+    if (rc != LZ_OK || left == 0) return rc;
+    a.wide_from = tiles - left;
+    return launch_ortho_narrow<KIND, PLANES>(a, left * 16, st);
+  }
+  const long long m = a.sp / kNarrow;
+  return launch_ortho_narrow<KIND, PLANES>(a, (kSym ? m * (m + 1) / 2 : m * (a.lp / kNarrow)) * a.n, st);
 }
 
 }  // namespace

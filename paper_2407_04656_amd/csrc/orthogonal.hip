@@ -138,6 +138,44 @@ __global__ __launch_bounds__(256) void load_kernel(Source s, OrthoSize z, const 
   }
 }
 
+// ... of wide matrices of whole aligned pieces: a piece of 8 a thread, without LDS (two 4096 x 14336 matrices 203 us there, 92 here).
+template <typename Elem, bool UPDATE, int PLANES>
+__global__ __launch_bounds__(256) void load_whole_kernel(Source s, OrthoSize z, const double* __restrict__ sums, int blocks, float eps,
+                                                         uint16_t* __restrict__ X) {
+  const float inv = inverse_norm(sums + (size_t)blockIdx.y * blocks, blocks, eps) * kOrthoScale;
+  const size_t base = (size_t)blockIdx.y * z.rows * z.cols, plane = (size_t)z.n * z.sp * z.lp;
+  uint16_t* const to = X + (size_t)blockIdx.y * z.sp * z.lp;
+  const int pieces = z.lp / 8;
+  for (size_t p = (size_t)blockIdx.x * 256 + threadIdx.x; p < (size_t)z.sp * pieces; p += (size_t)gridDim.x * 256) {
+    const int row = (int)(p / pieces), col = (int)(p - (size_t)row * pieces) * 8;
+    float v[8] = {};
+    if (row < z.rows && col < z.cols) {
+      const size_t at = base + (size_t)row * z.cols + col;
+      if constexpr (sizeof(Elem) == 4) {
+        *(f32x4*)v = *(const f32x4*)((const float*)s.g + at);
+        *(f32x4*)(v + 4) = *(const f32x4*)((const float*)s.g + at + 4);
+      } else {
+        const u32x4_t g = *(const u32x4_t*)((const uint16_t*)s.g + at);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[2 * e] = __uint_as_float(g[e] << 16);
+          v[2 * e + 1] = __uint_as_float(g[e] & 0xFFFF0000u);
+        }
+      }
+      if constexpr (UPDATE) {
+        float m[8];
+        *(f32x4*)m = *(const f32x4*)(s.momentum + at);
+        *(f32x4*)(m + 4) = *(const f32x4*)(s.momentum + at + 4);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = s.nesterov ? fmaf(s.mu, m[e], v[e]) : m[e];
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] *= inv;
+    }
+    store_planes8<PLANES>(to + (size_t)row * z.lp + col, plane, v);
+  }
+}
+
 // X -> the result as it lies; UPDATE: the weights, and their copies in the slots.
 template <typename Elem, bool UPDATE, int PLANES>
 __global__ __launch_bounds__(256) void finish_kernel(const uint16_t* __restrict__ X, OrthoSize z, Elem* __restrict__ out, Update u) {
@@ -278,6 +316,11 @@ int32_t run(const Source& source, const float* old, const lz_orthogonal_shape* s
            : sp == 64 ? run_thin<Elem, UPDATE, PLANES, 64>(source, z, steps, n_steps, eps, out, update, w, st)
                       : run_thin<Elem, UPDATE, PLANES, 128>(source, z, steps, n_steps, eps, out, update, w, st);
   }
+  if (whole && !z.tall && z.cols % 8 == 0) {
+    const unsigned blocks = (unsigned)((size_t)z.sp * z.lp / 8 / 256 + 1);
+    hipLaunchKernelGGL((load_whole_kernel<Elem, UPDATE, PLANES>), dim3(blocks < 8192 ? blocks : 8192, z.n), dim3(256), 0, st, source, z, w.sums, norms,
+                       eps, w.X[0]);
+  } else
   hipLaunchKernelGGL((load_kernel<Elem, UPDATE, PLANES>), dim3(tiles, z.n), dim3(256), 0, st, source, z, w.sums, norms, eps, w.X[0]);
   int32_t rc = lz::launch_status();
   int cur = 0;

@@ -350,24 +350,11 @@ inline int thin_parts(int n, int columns) {
   return most < kThinMostParts ? most : kThinMostParts;
 }
 
-// Lets a kernel have so much dynamic LDS; once per device (idempotent).
-template <auto KERNEL>
-int32_t thin_lds(int bytes) {
-  static std::atomic<bool> ready_on_device[kMaxDevices];
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return LZ_EHIP;
-  if (!ready_on_device[dev].load(std::memory_order_acquire)) {
-    if (hipFuncSetAttribute((const void*)KERNEL, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return LZ_EHIP;
-    ready_on_device[dev].store(true, std::memory_order_release);
-  }
-  return LZ_OK;
-}
-
 template <typename Elem, bool UPDATE, int MODE, int SP, int PLANES>
 int32_t launch_thin(const ThinArgs& a, const Source& source, const OrthoSize& z, void* out, const Update& u, hipStream_t st) {
   constexpr auto kern = thin_step_kernel<Elem, UPDATE, MODE, SP, PLANES>;
   constexpr int kLds = ThinLds<SP, PLANES>::bytes;
-  const int32_t rc = thin_lds<kern>(kLds);
+  const int32_t rc = allow_lds<kern>(kLds);
   if (rc != LZ_OK) return rc;
   hipLaunchKernelGGL(kern, dim3(a.parts, z.n), dim3(kThinThreads<SP>), kLds, st, a, source, z, (Elem*)out, u);
   return lz::launch_status();

@@ -89,7 +89,8 @@ def test_orthogonalize(size, dtype, kind):
 
 
 # as many tiles as the wide kernel takes, whole ones and of 64, 128 and 192 rows; several bands of them
-WIDE = [(40, 300, 500), (36, 330, 440), (34, 380, 400), (7, 1090, 1150), (11, 1300, 770)]
+# and a few tiles more than the chip has places
+WIDE = [(90, 300, 330), (70, 290, 500), (40, 300, 500), (36, 330, 440), (34, 380, 400), (7, 1090, 1150), (11, 1300, 770)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
