@@ -168,7 +168,9 @@ __global__ __launch_bounds__(kOrthoThreads, 4) void ortho_narrow_kernel(OrthoArg
   };
   for (int kt = 0; kt < all_steps; ++kt) {
     constexpr int kAhead = (NS - 2) * kLoads;
-    __builtin_amdgcn_s_waitcnt(0x0F70 | (kAhead & 15) | ((kAhead >> 4) << 14));  // this wave's loads of step kt are in LDS
+    // this wave's loads of step kt are in LDS, and its fragments of step kt - 1, used below only, in registers (lgkmcnt 0): the next loads
+    // go where they lay
+    __builtin_amdgcn_s_waitcnt(0x0070 | (kAhead & 15) | ((kAhead >> 4) << 14));
     __syncthreads();  // ... everyone's are; and nobody reads the stage of step kt - 1 any more
     issue(kt + NS - 1 < all_steps, stage == 0 ? NS - 1 : stage - 1);
     const char* const st = smem + stage * kNarrowStage;

@@ -148,6 +148,19 @@ def test_in_place_and_unaligned(size, dtype):
     assert torch.equal(view, want)
 
 
+@pytest.mark.parametrize("size,dtype", [((32, 1344, 256), BF16), ((50, 256, 192), BF16), ((61, 1024, 256), F32), ((8, 768, 1664), F32),
+                                        ((40, 24, 600), F32), ((9, 100, 900), BF16)])
+def test_same_bits_every_time(size, dtype):
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    g = torch.randn(size, generator=gen, device=DEV).to(torch.float32 if dtype == F32 else torch.bfloat16)
+    u = lz.OrthogonalUpdate(lz.OrthogonalShape(*size, dtype), DEV)
+    want = u.orthogonalize(g).clone()
+    differ = torch.zeros((), dtype=torch.int64, device=DEV)
+    for _ in range(300):
+        differ += (u.orthogonalize(g) != want).sum()
+    assert int(differ.item()) == 0
+
+
 STEPS = [((3, 100, 70), 5), ((2, 16, 300), 2), ((4, 64, 64), 9), ((1, 9, 1), 0), ((5, 130, 260), 70), ((2, 300, 130), 3)]
 
 
