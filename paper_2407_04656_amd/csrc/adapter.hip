@@ -50,7 +50,25 @@ inline int factor_chunk(int T) {
 }
 inline int factor_units(const lz_adapter_shape* s) { return s->T / factor_chunk(s->T) + s->n; }
 
+// fp32 sizes that are no whole 16-byte pieces are copied to the next ones that are, with zeros around them, where the products are large
+// enough to pay for it: by single elements the products run at 25 to 30 TFLOP/s.  11575 x 1967 x 1325, rank 14: 1228 us by elements,
+// PADUS so; 1021 x 500 x 1301 67 and 61.
+inline int up4(int v) { return (v + 3) / 4 * 4; }
+inline bool padded(const lz_adapter_shape* s) {
+  return s->dtype == LZ_F32 && (s->d_in % 4 != 0 || s->d_out % 4 != 0 || s->rank % 4 != 0) && s->T >= 256 &&
+         (long long)s->T * s->d_in * s->d_out >= 100000000ll;
+}
+inline lz_adapter_shape computed_shape(const lz_adapter_shape* s) {
+  lz_adapter_shape p = *s;
+  if (padded(s)) p.d_in = up4(s->d_in), p.d_out = up4(s->d_out), p.rank = up4(s->rank);
+  return p;
+}
+struct PaddedTensors {
+  float *x, *w, *a, *b, *h, *y, *dy, *dx, *da, *db;
+};
+
 struct AdapterWorkspace {
+  PaddedTensors pad;
   int32_t* ids;      // [T], -1: none
   int32_t* counts;   // [chunks, n + 1], then where a chunk's tokens of an adapter go, from the adapter's first row on
   int32_t* first;    // [n + 2]: first row of every adapter, of the tokens without one, T
@@ -72,8 +90,9 @@ struct AdapterWorkspace {
   size_t bytes;
 };
 
-AdapterWorkspace carve(void* ws, const lz_adapter_shape* s) {
+AdapterWorkspace carve(void* ws, const lz_adapter_shape* given) {
   AdapterWorkspace w{};
+  const lz_adapter_shape computed = computed_shape(given), *const s = &computed;
   char* p = (char*)ws;
   auto take = [&](size_t bytes) {
     char* r = p;
@@ -121,8 +140,41 @@ AdapterWorkspace carve(void* ws, const lz_adapter_shape* s) {
     w.factor_part[1] = (float*)take(4 * units * s->rank * s->d_out);
     w.at = (uint16_t*)take(2 * (size_t)s->n * s->rank * s->d_in);
   }
+  if (padded(given)) {
+    const size_t low = (size_t)s->n * s->rank;
+    auto floats = [&](size_t n) { return (float*)take(4 * n); };
+    w.pad = PaddedTensors{floats(T * s->d_in), floats((size_t)s->d_in * s->d_out), floats(low * s->d_in), floats(low * s->d_out), floats(T * s->rank),
+                          floats(T * s->d_out), floats(T * s->d_out), floats(T * s->d_in), floats(low * s->d_in), floats(low * s->d_out)};
+  }
   w.bytes = size_t(p - (char*)ws);
   return w;
+}
+
+// Matrices [count][rows][cols] copied to [count][to_rows][to_cols], with zeros where that is larger; blockIdx.y = job, a wave a row.
+struct CopyJob {
+  const float* from;
+  float* to;
+  int count, rows, cols, to_rows, to_cols;
+};
+struct CopyJobs {
+  CopyJob job[6];
+};
+__global__ __launch_bounds__(256) void copy_jobs_kernel(CopyJobs jobs) {
+  const CopyJob j = jobs.job[blockIdx.y];
+  const long long all = (long long)j.count * j.to_rows;
+  for (long long r = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); r < all; r += (long long)gridDim.x * 4) {
+    const int m = (int)(r / j.to_rows), row = (int)(r - (long long)m * j.to_rows);
+    const float* const from = j.from + ((size_t)m * j.rows + row) * j.cols;
+#pragma unroll 4
+    for (int c = threadIdx.x & 63; c < j.to_cols; c += 64) j.to[(size_t)r * j.to_cols + c] = row < j.rows && c < j.cols ? from[c] : 0.f;
+  }
+}
+int32_t copy_jobs(std::initializer_list<CopyJob> list, hipStream_t st) {
+  CopyJobs jobs{};
+  int n = 0;
+  for (const CopyJob& j : list) jobs.job[n++] = j;
+  hipLaunchKernelGGL(copy_jobs_kernel, dim3(1024, n), dim3(256), 0, st, jobs);
+  return lz::launch_status();
 }
 
 __global__ __launch_bounds__(64) void count_ids_kernel(const int32_t* __restrict__ ids, int T, int n, int chunk, int32_t* __restrict__ clean,
@@ -470,14 +522,15 @@ int32_t sort_with_tables(const AdapterWorkspace& w, const lz_adapter_shape* s, h
 
 // ---- bf16 kernels
 
-// One token's rows are read by its own wave where tokens are few: an adapter after the other costs a workgroup of 16 a trip each.
-constexpr int kFewTokens = 128;
+// A token's adapter is read by its own waves where that is up to 64 MB in all: the tile kernel takes the adapters of 64 tokens one after
+// the other.  252 tokens of as many requests, 105 adapters of rank 8, 2048 x 3392: a training step 368 us by tiles, 129 so.
+inline bool by_token(const lz_adapter_shape* s, int d) { return (long long)s->T * s->rank * d <= (32ll << 20) && s->T <= 65535; }
 
 int32_t low_rank_mfma(const AdapterWorkspace& w, const lz_adapter_shape* s, const void* x, int d, const void* a, const float* scale, void* h,
                       hipStream_t st) {
   LowRankArgs args{(const uint16_t*)x, (const uint16_t*)a, scale, w.ids, w.lists.count64, w.lists.list64, w.lists.local64,
                    (uint16_t*)h, w.low, s->T, d, s->rank, low_rank_splits(s, d)};
-  if (s->T <= kFewTokens) {
+  if (by_token(s, d)) {
     hipLaunchKernelGGL(low_rank_token_kernel, dim3(s->T, ceil_div(s->rank, 4)), dim3(256), 0, st, args);
     return lz::launch_status();
   }
@@ -589,6 +642,15 @@ extern "C" int32_t lz_adapter_forward(const void* x, const void* w, const void* 
     const int32_t sorted = sort_with_tables(m, shape, st);
     if (sorted != LZ_OK) return sorted;
   }
+  if (padded(shape)) {
+    const lz_adapter_shape p = computed_shape(shape);
+    const PaddedTensors& t = m.pad;
+    const int T = shape->T, n = shape->n, r = shape->rank, in = shape->d_in, out = shape->d_out;
+    int32_t rc = copy_jobs({{(const float*)x, t.x, 1, T, in, T, p.d_in}, {(const float*)w, t.w, 1, in, out, p.d_in, p.d_out},
+                            {(const float*)a, t.a, n, r, in, p.rank, p.d_in}, {(const float*)b, t.b, n, r, out, p.rank, p.d_out}}, st);
+    if (rc == LZ_OK) rc = forward<float>(m, &p, t.x, t.w, t.a, t.b, scale, t.h, t.y, st);
+    return rc == LZ_OK ? copy_jobs({{t.y, (float*)y, 1, T, p.d_out, T, out}, {t.h, (float*)h, 1, T, p.rank, T, r}}, st) : rc;
+  }
   return shape->dtype == LZ_F32 ? forward<float>(m, shape, x, w, a, b, scale, h, y, st)
                                 : forward<uint16_t>(m, shape, x, w, a, b, scale, h, y, st);
 }
@@ -616,6 +678,17 @@ extern "C" int32_t lz_adapter_backward(const void* dy, const void* x, const void
     if (all16({dy, x, h, w, a, b, dx, da, db})) return backward_mfma(m, shape, dy, x, h, w, a, b, scale, dx, da, db, st);
     const int32_t sorted = sort_with_tables(m, shape, st);
     if (sorted != LZ_OK) return sorted;
+  }
+  if (padded(shape)) {
+    const lz_adapter_shape p = computed_shape(shape);
+    const PaddedTensors& t = m.pad;
+    const int T = shape->T, n = shape->n, r = shape->rank, in = shape->d_in, out = shape->d_out;
+    int32_t rc = copy_jobs({{(const float*)x, t.x, 1, T, in, T, p.d_in}, {(const float*)w, t.w, 1, in, out, p.d_in, p.d_out},
+                            {(const float*)a, t.a, n, r, in, p.rank, p.d_in}, {(const float*)b, t.b, n, r, out, p.rank, p.d_out},
+                            {(const float*)dy, t.dy, 1, T, out, T, p.d_out}, {(const float*)h, t.h, 1, T, r, T, p.rank}}, st);
+    if (rc == LZ_OK) rc = backward<float>(m, &p, t.dy, t.x, t.h, t.w, t.a, t.b, scale, t.dx, t.da, t.db, st);
+    if (rc != LZ_OK) return rc;
+    return copy_jobs({{t.dx, (float*)dx, 1, T, p.d_in, T, in}, {t.da, (float*)da, n, p.rank, p.d_in, r, in}, {t.db, (float*)db, n, p.rank, p.d_out, r, out}}, st);
   }
   return shape->dtype == LZ_F32 ? backward<float>(m, shape, dy, x, h, w, a, b, scale, dx, da, db, st)
                                 : backward<uint16_t>(m, shape, dy, x, h, w, a, b, scale, dx, da, db, st);

@@ -22,16 +22,19 @@ constexpr float kOrthoScale = 16384.f;
 
 enum { KIND_GRAM = 0, KIND_SQUARE = 1, KIND_APPLY = 2 };
 
+constexpr int kMostParts = 512;
 struct OrthoArgs {
   const uint16_t* X;  // [planes][n][sp][lp]
   uint16_t* H;        // [planes][n][sp][sp]
   uint16_t* P;        // ...
   uint16_t* out;      // APPLY: X'
   float* residual;    // [n][sp]: what rounding took from H's diagonal (one plane)
+  float* part;        // GRAM: [splits][tiles][64][64], at most kMostParts of them
   int n, sp, lp;
   float mu, c2, lin, diag, rho;  // diag = q0 - rho
   int pairs;                     // of planes that a product of two planes sums: 3, or 1: hi hi alone
   int tiles = 0;                 // of the launch
+  int splits = 1;                // GRAM: workgroups that share a tile's sum
   int wide_from = -1;            // >= 0: they are those of the wide kernel's from here on, 16 each
 };
 
@@ -62,36 +65,20 @@ __device__ __forceinline__ void load_planes8(const uint16_t* from, size_t plane,
   }
 }
 
-// 64 x 64 tiles, a ring of four K steps of 64 as in gemm_narrow.h; eight waves of 32 x 32, either four of which take half of a step's k
-// and add up through LDS at the end, a step's products while the next one's fragments are on their way.  A step takes 0.3 us, a quarter of
-// it products: 16 KB into LDS and 32 KB out of it, one after the other at a barrier.  Four waves of all k, fragments without the
-// step ahead, and a ring of eight steps were within 7 % of this.
-// GRAM and SQUARE are symmetric: only tiles
-// on and below the diagonal are computed, and stored twice.  A launch takes all tiles, or
-// what is left of a wide one's (a.wide_from).
-constexpr int kOrthoThreads = 512;
-template <int KIND, int PLANES>
-__global__ __launch_bounds__(kOrthoThreads, 4) void ortho_narrow_kernel(OrthoArgs a) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  constexpr bool TB = KIND == KIND_APPLY;  // W k-major
-  constexpr int NS = kNarrowStages, kLoads = 2;
-  extern __shared__ __attribute__((aligned(1024))) char smem[];
+// A narrow tile of a launch: false if it is none (of what is left of a wide launch, beyond an edge or above the diagonal).
+template <bool TB>
+__device__ __forceinline__ bool ortho_place(const OrthoArgs& a, int index, int& matrix, int& tm, int& tn) {
   const int sp = a.sp, lp = a.lp;
-  // Workgroups are dealt to the 8 XCDs in turn: each XCD has a run of the tiles, which share panels in its L2 (dealt in turn, APPLY
-  // of five 777 x 333 matrices in two planes takes 14.8 us, so 13.3).
-  const int at_xcd = (int)((long long)a.tiles * (blockIdx.x % 8) / 8) + (int)(blockIdx.x / 8);
-  if (at_xcd >= (int)((long long)a.tiles * (blockIdx.x % 8 + 1) / 8)) return;
-  int tm, tn, matrix;
   if (a.wide_from >= 0) {  // 16 tiles of a wide one
-    const FixedTile t = fixed_tile<!TB>(a.wide_from + at_xcd / 16, (sp + BM - 1) / BM, (lp + BN - 1) / BN);
+    const FixedTile t = fixed_tile<!TB>(a.wide_from + index / 16, (sp + BM - 1) / BM, (lp + BN - 1) / BN);
     matrix = t.matrix;
-    tm = t.row * 4 + at_xcd / 4 % 4;
-    tn = t.col * 4 + at_xcd % 4;
-    if (tm >= sp / kNarrow || tn >= (TB ? lp : sp) / kNarrow || (!TB && tn > tm)) return;
+    tm = t.row * 4 + index / 4 % 4;
+    tn = t.col * 4 + index % 4;
+    if (tm >= sp / kNarrow || tn >= (TB ? lp : sp) / kNarrow || (!TB && tn > tm)) return false;
   } else {
     const int m = sp / kNarrow, each = TB ? m * (lp / kNarrow) : m * (m + 1) / 2;
-    matrix = at_xcd / each;
-    const int t = at_xcd - matrix * each;
+    matrix = index / each;
+    const int t = index - matrix * each;
     if constexpr (TB) {
       const int cols = lp / kNarrow;
       tm = t / cols;
@@ -106,6 +93,78 @@ __global__ __launch_bounds__(kOrthoThreads, 4) void ortho_narrow_kernel(OrthoArg
     tm = __builtin_amdgcn_readfirstlane(tm);
     tn = __builtin_amdgcn_readfirstlane(tn);
   }
+  return true;
+}
+
+// A tile's sums, [row][column] in LDS, to the result, by kOrthoThreads threads.
+constexpr int kOrthoThreads = 512, kOrthoPitch = kNarrow + 1;
+template <int KIND, int PLANES>
+__device__ __forceinline__ void finish_ortho_tile(const OrthoArgs& a, const float* tile, int matrix, int tm, int tn) {
+  constexpr int kPitch = kOrthoPitch;
+  constexpr float kDown = 1.f / kOrthoScale;
+  const int sp = a.sp, lp = a.lp, m0 = tm * kNarrow, n0 = tn * kNarrow;
+  const size_t large = (size_t)sp * lp, small = (size_t)sp * sp, at = matrix, planeA = small * a.n, planeW = large * a.n;
+  {
+    const int r = threadIdx.x >> 3, c = (threadIdx.x & 7) * 8;
+    float v[8];
+    if constexpr (KIND == KIND_APPLY) {
+      const size_t to = at * large + (size_t)(m0 + r) * lp + n0 + c;
+      float x[8];
+      load_planes8<PLANES>(a.X + to, planeW, x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = fmaf(a.rho, x[j], tile[r * kPitch + c + j] * kDown);
+      store_planes8<PLANES>(a.out + to, planeW, v);
+    } else {
+      // value of element (row, column) of the tile; `from`: of H, where it is read
+      auto finish = [&](float sum, int row, int col, float h) {
+        const bool on = m0 + row == n0 + col;
+        if constexpr (KIND == KIND_GRAM) return fmaf(sum, kDown, on ? -a.mu * kOrthoScale : 0.f);
+        if (PLANES == 1 && on) sum = fmaf(2.f * a.residual[at * sp + m0 + row], h, sum);
+        return fmaf(a.lin, h, fmaf(a.c2 * kDown, sum, on ? a.diag * kOrthoScale : 0.f));
+      };
+      const size_t to = at * small + (size_t)(m0 + r) * sp + n0 + c;
+      const bool with_h = KIND == KIND_SQUARE && (a.lin != 0.f || tm == tn);
+      uint16_t* const dst = KIND == KIND_GRAM ? a.H : a.P;
+      float h[8] = {};
+      if (with_h) load_planes8<PLANES>(a.H + to, planeA, h);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        v[j] = finish(tile[r * kPitch + c + j], r, c + j, h[j]);
+        if (KIND == KIND_GRAM && PLANES == 1 && m0 + r == n0 + c + j) a.residual[at * sp + m0 + r] = v[j] - f16_value(f16_bits(v[j]));
+      }
+      store_planes8<PLANES>(dst + to, KIND == KIND_GRAM ? small * a.n : planeA, v);
+      if (tm != tn) {
+        const size_t mirror = at * small + (size_t)(n0 + r) * sp + m0 + c;
+        if (with_h) load_planes8<PLANES>(a.H + mirror, planeA, h);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = finish(tile[(c + j) * kPitch + r], c + j, r, h[j]);
+        store_planes8<PLANES>(dst + mirror, KIND == KIND_GRAM ? small * a.n : planeA, v);
+      }
+    }
+  }
+}
+
+// 64 x 64 tiles, a ring of four K steps of 64 as in gemm_narrow.h; eight waves of 32 x 32, either four of which take half of a step's k
+// and add up through LDS at the end, a step's products while the next one's fragments are on their way.  A step takes 0.3 us, a quarter of
+// it products: 16 KB into LDS and 32 KB out of it, one after the other at a barrier.  Four waves of all k, fragments without the
+// step ahead, and a ring of eight steps were within 7 % of this.
+// GRAM and SQUARE are symmetric: only tiles
+// on and below the diagonal are computed, and stored twice.  A launch takes all tiles, or
+// what is left of a wide one's (a.wide_from).
+template <int KIND, int PLANES>
+__global__ __launch_bounds__(kOrthoThreads, 4) void ortho_narrow_kernel(OrthoArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr bool TB = KIND == KIND_APPLY;  // W k-major
+  constexpr int NS = kNarrowStages, kLoads = 2;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int sp = a.sp, lp = a.lp;
+  // Workgroups are dealt to the 8 XCDs in turn: each XCD has a run of the tiles, which share panels in its L2 (dealt in turn, APPLY
+  // of five 777 x 333 matrices in two planes takes 14.8 us, so 13.3).
+  const int all = a.tiles * a.splits, mine = (int)((long long)all * (blockIdx.x % 8) / 8) + (int)(blockIdx.x / 8);
+  if (mine >= (int)((long long)all * (blockIdx.x % 8 + 1) / 8)) return;
+  const int index = KIND == KIND_GRAM ? __builtin_amdgcn_readfirstlane(mine / a.splits) : mine, split = mine - index * a.splits;
+  int tm, tn, matrix;
+  if (!ortho_place<TB>(a, index, matrix, tm, tn)) return;
   const int m0 = tm * kNarrow, n0 = tn * kNarrow;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int ks = wave >> 2, wm = (wave >> 1) & 1, wn = wave & 1;
@@ -121,8 +180,10 @@ __global__ __launch_bounds__(kOrthoThreads, 4) void ortho_narrow_kernel(OrthoArg
   const int voffX = (int)(((uint32_t)(m0 + load_row) * (uint32_t)K + (uint32_t)load_chunk * 8u) * 2u);
   const int voffW = TB ? (int)(((uint32_t)load_row * (uint32_t)ldw + (uint32_t)(n0 + ((lane & 7) ^ swz_narrow(load_row)) * 8)) * 2u)
                        : (int)(((uint32_t)(n0 + load_row) * (uint32_t)K + (uint32_t)load_chunk * 8u) * 2u);
-  const int k_steps = K / BK, all_steps = PLANES == 2 ? a.pairs * k_steps : k_steps;
-  int seg = 0, k = 0;  // of the next step to load: which pair of planes, step within it
+  const int k_steps = K / BK, whole_steps = PLANES == 2 ? a.pairs * k_steps : k_steps;
+  const int step0 = KIND == KIND_GRAM ? (int)((long long)whole_steps * split / a.splits) : 0;
+  const int all_steps = KIND == KIND_GRAM ? (int)((long long)whole_steps * (split + 1) / a.splits) - step0 : whole_steps;
+  int seg = __builtin_amdgcn_readfirstlane(step0 / k_steps), k = step0 - seg * k_steps;  // of the next step to load: which pair of planes, step within it
   auto issue = [&](bool real, int stage) {  // a step past the end writes zeros, without memory traffic
     const i32x4 wa = rsrc_words(matA + (seg == 2 ? planeA : 0), real ? extentA : 0), ww = rsrc_words(matW + (seg == 1 ? planeW : 0), real ? extentW : 0);
     const uint32_t lds = lds0 + stage * kNarrowStage + wave * 1024;
@@ -189,7 +250,7 @@ __global__ __launch_bounds__(kOrthoThreads, 4) void ortho_narrow_kernel(OrthoArg
   __builtin_amdgcn_s_waitcnt(0x0F70);
   __syncthreads();
   // the tile, fp32, [row][column] through LDS, so that both it and its mirror image leave in 16-byte pieces
-  constexpr int kPitch = kNarrow + 1;
+  constexpr int kPitch = kOrthoPitch;
   float* const tile = (float*)smem;
   auto each = [&](auto what) {
 #pragma unroll
@@ -204,45 +265,14 @@ __global__ __launch_bounds__(kOrthoThreads, 4) void ortho_narrow_kernel(OrthoArg
   __syncthreads();
   if (ks == 1) each([](float& to, float v) { to += v; });
   __syncthreads();
-  constexpr float kDown = 1.f / kOrthoScale;
-  {
+  if (KIND == KIND_GRAM && a.splits > 1) {
     const int r = threadIdx.x >> 3, c = (threadIdx.x & 7) * 8;
-    float v[8];
-    if constexpr (KIND == KIND_APPLY) {
-      const size_t to = at * large + (size_t)(m0 + r) * lp + n0 + c;
-      float x[8];
-      load_planes8<PLANES>(a.X + to, planeW, x);
+    float* const to = a.part + ((size_t)split * a.tiles + index) * (kNarrow * kNarrow) + r * kNarrow + c;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = fmaf(a.rho, x[j], tile[r * kPitch + c + j] * kDown);
-      store_planes8<PLANES>(a.out + to, planeW, v);
-    } else {
-      // value of element (row, column) of the tile; `from`: of H, where it is read
-      auto finish = [&](float sum, int row, int col, float h) {
-        const bool on = m0 + row == n0 + col;
-        if constexpr (KIND == KIND_GRAM) return fmaf(sum, kDown, on ? -a.mu * kOrthoScale : 0.f);
-        if (PLANES == 1 && on) sum = fmaf(2.f * a.residual[at * sp + m0 + row], h, sum);
-        return fmaf(a.lin, h, fmaf(a.c2 * kDown, sum, on ? a.diag * kOrthoScale : 0.f));
-      };
-      const size_t to = at * small + (size_t)(m0 + r) * sp + n0 + c;
-      const bool with_h = KIND == KIND_SQUARE && (a.lin != 0.f || tm == tn);
-      uint16_t* const dst = KIND == KIND_GRAM ? a.H : a.P;
-      float h[8] = {};
-      if (with_h) load_planes8<PLANES>(a.H + to, planeA, h);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        v[j] = finish(tile[r * kPitch + c + j], r, c + j, h[j]);
-        if (KIND == KIND_GRAM && PLANES == 1 && m0 + r == n0 + c + j) a.residual[at * sp + m0 + r] = v[j] - f16_value(f16_bits(v[j]));
-      }
-      store_planes8<PLANES>(dst + to, KIND == KIND_GRAM ? small * a.n : planeA, v);
-      if (tm != tn) {
-        const size_t mirror = at * small + (size_t)(n0 + r) * sp + m0 + c;
-        if (with_h) load_planes8<PLANES>(a.H + mirror, planeA, h);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = finish(tile[(c + j) * kPitch + r], c + j, r, h[j]);
-        store_planes8<PLANES>(dst + mirror, KIND == KIND_GRAM ? small * a.n : planeA, v);
-      }
-    }
+    for (int j = 0; j < 8; ++j) to[j] = tile[r * kPitch + c + j];
+    return;
   }
+  finish_ortho_tile<KIND, PLANES>(a, tile, matrix, tm, tn);
 #endif
 }
 
@@ -281,12 +311,43 @@ int32_t launch_ortho_wide(const OrthoArgs& a, int tiles, hipStream_t st) {
   return launch_mfma_kernel<kEpi, KIND == KIND_APPLY ? MODE_NN : MODE_NT, false, false, false>(MfmaLaunch<false>{{g}}, st);
 }
 
+// The splits' sums, added in fp32 in their order.  A workgroup per tile.
+template <int PLANES>
+__global__ __launch_bounds__(kOrthoThreads) void join_gram_kernel(OrthoArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __shared__ float tile[kNarrow * kOrthoPitch];
+  const int r = threadIdx.x >> 3, c = (threadIdx.x & 7) * 8;
+  int matrix, tm, tn;
+  if (!ortho_place<false>(a, blockIdx.x, matrix, tm, tn)) return;
+  const float* from = a.part + (size_t)blockIdx.x * (kNarrow * kNarrow) + r * kNarrow + c;
+  f32x4 v0 = {}, v1 = {};
+#pragma unroll 4
+  for (int s = 0; s < a.splits; ++s, from += (size_t)a.tiles * (kNarrow * kNarrow)) {
+    v0 += *(const f32x4*)from;
+    v1 += *(const f32x4*)(from + 4);
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) tile[r * kOrthoPitch + c + j] = v0[j], tile[r * kOrthoPitch + c + 4 + j] = v1[j];
+  __syncthreads();
+  finish_ortho_tile<KIND_GRAM, PLANES>(a, tile, matrix, tm, tn);
+#endif
+}
+
+// GRAM of few matrices has few tiles and a long sum: so many workgroups share a tile that the chip's places are taken, with 16 steps
+// each at least (a step of one 448 x 7488 matrix in two planes, 28 tiles of 351 steps, 547 us without, SPLITUS so).
 template <int KIND, int PLANES>
 int32_t launch_ortho_narrow(OrthoArgs a, long long tiles, hipStream_t st) {
   if (tiles > 0x7FFFFFF0ll) return LZ_ESHAPE;
   a.tiles = (int)tiles;
-  const dim3 grid((unsigned)((tiles + 7) / 8 * 8)), threads(kOrthoThreads);
-  hipLaunchKernelGGL((ortho_narrow_kernel<KIND, PLANES>), grid, threads, kNarrowLds, st, a);
+  if (KIND == KIND_GRAM) {
+    const int steps = a.lp / BK * (PLANES == 2 ? a.pairs : 1);
+    const long long fill = kMostParts / tiles, most = steps / 16;
+    a.splits = (int)(fill < most ? fill : most);
+    if (a.splits < 2) a.splits = 1;
+  }
+  const unsigned all = (unsigned)(a.tiles * a.splits);
+  hipLaunchKernelGGL((ortho_narrow_kernel<KIND, PLANES>), dim3((all + 7) / 8 * 8), dim3(kOrthoThreads), kNarrowLds, st, a);
+  if (KIND == KIND_GRAM && a.splits > 1) hipLaunchKernelGGL((join_gram_kernel<PLANES>), dim3(a.tiles), dim3(kOrthoThreads), 0, st, a);
   return lz::launch_status();
 }
 

@@ -20,11 +20,19 @@ inline bool shape_ok(const lz_orthogonal_shape* s) {
 
 inline int small_side(const lz_orthogonal_shape* s) { return s->rows < s->cols ? s->rows : s->cols; }
 
+// A step in one launch pays where launches are what bounds it.  Sides of 65 to 128 hold a CU's LDS alone there: past 1024 blocks of
+// columns bf16 matrices run as wider ones do (48 of 75 x 3587, a step of fp32 weights: 852 us thin, THINUS so); fp32 ones stay, whose
+// long sums are the more exact there.
+inline bool use_thin(const lz_orthogonal_shape* s) {
+  const int small = small_side(s), large = s->rows < s->cols ? s->cols : s->rows;
+  return small <= kThinMost && (small <= 64 || s->dtype == LZ_F32 || (long long)s->n * (up64(large) / kThinBlock) <= 1024);
+}
+
 struct OrthoWorkspace {
   double* sums;     // [n, norm_blocks()]
   float* residual;  // [n, sp]
   uint16_t *X[2], *H, *P;  // two planes each; thin matrices: X column by column
-  float* part[2];          // thin matrices: parts of G
+  float* part[2];          // thin matrices: parts of G; the others, the first: those of GRAM's sums
   size_t bytes;
 };
 OrthoWorkspace carve(void* ws, const lz_orthogonal_shape* s) {
@@ -38,7 +46,7 @@ OrthoWorkspace carve(void* ws, const lz_orthogonal_shape* s) {
   };
   w.sums = (double*)take(sizeof(double) * z.n * norm_blocks((size_t)z.rows * z.cols));
   w.residual = (float*)take(sizeof(float) * z.n * z.sp);
-  if (small_side(s) <= kThinMost) {
+  if (use_thin(s)) {
     const int sp = thin_side(small_side(s));
     for (auto& x : w.X) x = (uint16_t*)take(4 * (size_t)z.n * sp * z.lp);
     for (auto& g : w.part) g = (float*)take(4 * (size_t)z.n * thin_parts(z.n, z.lp) * sp * sp);
@@ -48,6 +56,7 @@ OrthoWorkspace carve(void* ws, const lz_orthogonal_shape* s) {
   for (auto& x : w.X) x = (uint16_t*)take(4 * (size_t)z.n * z.sp * z.lp);
   w.H = (uint16_t*)take(4 * (size_t)z.n * z.sp * z.sp);
   w.P = (uint16_t*)take(4 * (size_t)z.n * z.sp * z.sp);
+  w.part[0] = (float*)take(4 * (size_t)kMostParts * kNarrow * kNarrow);
   w.bytes = size_t(p - (char*)ws);
   return w;
 }
@@ -244,8 +253,7 @@ struct Step {
 //
 // Thin matrices have no square to save: while most directions are small, H = G holds what they are off 0 by with all its bits, where
 // G - mu would be mu and little else (70 x 33 x 40 of a few large directions, two planes: 6e-6 of the result with mu throughout).
-bool plan_steps(const float* coef, int steps, int planes, int small, bool update, Step* out) {
-  const bool thin = small <= kThinMost;
+bool plan_steps(const float* coef, int steps, int planes, int small, bool thin, bool update, Step* out) {
   double most = 1.0, typical = 1.0 / small;
   for (int k = 0; k < steps; ++k) {
     const double a = coef[3 * k], b = coef[3 * k + 1], c = coef[3 * k + 2];
@@ -308,10 +316,10 @@ int32_t run(const Source& source, const float* old, const lz_orthogonal_shape* s
   const int norms = norm_blocks(elems);
   const bool whole = elems % 8 == 0 && aligned16(source.g) && aligned16(old) && aligned16(source.momentum);
   hipLaunchKernelGGL((norm_kernel<Elem, UPDATE>), dim3(norms, z.n), dim3(256), 0, st, source, old, (float*)source.momentum, elems, whole, w.sums);
-  if (const int small = small_side(shape); small <= kThinMost) {
+  if (use_thin(shape)) {
     const int32_t rc = lz::launch_status();
     if (rc != LZ_OK) return rc;
-    const int sp = thin_side(small);
+    const int sp = thin_side(small_side(shape));
     return sp == 32   ? run_thin<Elem, UPDATE, PLANES, 32>(source, z, steps, n_steps, eps, out, update, w, st)
            : sp == 64 ? run_thin<Elem, UPDATE, PLANES, 64>(source, z, steps, n_steps, eps, out, update, w, st)
                       : run_thin<Elem, UPDATE, PLANES, 128>(source, z, steps, n_steps, eps, out, update, w, st);
@@ -326,7 +334,7 @@ int32_t run(const Source& source, const float* old, const lz_orthogonal_shape* s
   int cur = 0;
   for (int k = 0; k < n_steps && rc == LZ_OK; ++k, cur ^= 1) {
     const Step& s = steps[k];
-    const OrthoArgs a{w.X[cur], w.H, w.P, w.X[cur ^ 1], w.residual, z.n, z.sp, z.lp, s.mu, s.c2, s.lin, s.diag, s.rho, s.coarse ? 1 : 3};
+    const OrthoArgs a{w.X[cur], w.H, w.P, w.X[cur ^ 1], w.residual, w.part[0], z.n, z.sp, z.lp, s.mu, s.c2, s.lin, s.diag, s.rho, s.coarse ? 1 : 3};
     rc = s.coarse ? launch_ortho<KIND_GRAM, 1>(a, st) : launch_ortho<KIND_GRAM, PLANES>(a, st);
     if (rc == LZ_OK) rc = s.coarse ? launch_ortho<KIND_SQUARE, 1>(a, st) : launch_ortho<KIND_SQUARE, PLANES>(a, st);
     if (rc == LZ_OK) rc = launch_ortho<KIND_APPLY, PLANES>(a, st);
@@ -339,7 +347,7 @@ int32_t run(const Source& source, const float* old, const lz_orthogonal_shape* s
 int32_t check(const lz_orthogonal_shape* s, const float* coef, int32_t steps, float eps, int planes, bool update, void* ws, size_t ws_bytes, OrthoWorkspace* w,
               Step* plan) {
   if (!shape_ok(s)) return LZ_ESHAPE;
-  if (!coef || steps < 1 || steps > kMostSteps || !(eps >= 0.f) || !std::isfinite(eps) || !plan_steps(coef, steps, planes, small_side(s), update, plan)) return LZ_EINVAL;
+  if (!coef || steps < 1 || steps > kMostSteps || !(eps >= 0.f) || !std::isfinite(eps) || !plan_steps(coef, steps, planes, small_side(s), use_thin(s), update, plan)) return LZ_EINVAL;
   *w = carve(ws, s);
   if (!ws || (uintptr_t)ws % 256 != 0 || ws_bytes < w->bytes) return LZ_EWORKSPACE;
   return LZ_OK;

@@ -34,6 +34,8 @@ ODD = [  # sizes that only single elements fit
     (1021, 100, 261, 12, 9, 9, 0.2),
     (4200, 33, 20, 3, 50, 700, 0.1),
     (300, 20, 36, 4, 1500, 300, 0.1),
+    (700, 401, 379, 6, 5, 20, 0.2),
+    (513, 444, 447, 9, 3, 3, 0.0),
 ]
 
 

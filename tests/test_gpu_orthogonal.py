@@ -73,7 +73,8 @@ def allowed(u, coef, planes, dtype):
 
 # n, rows, cols
 SIZES = [(1, 1, 1), (3, 1, 7), (2, 5, 1), (4, 8, 64), (2, 64, 8), (1, 63, 65), (2, 65, 63), (3, 100, 130), (2, 130, 100), (1, 128, 1000),
-         (2, 16, 4096), (1, 4096, 16), (8, 128, 256), (2, 200, 777), (1, 777, 333), (1, 320, 320), (70, 33, 40), (1, 520, 1300)]
+         (2, 16, 4096), (1, 4096, 16), (8, 128, 256), (2, 200, 777), (1, 777, 333), (1, 320, 320), (70, 33, 40), (1, 520, 1300),
+         (64, 100, 1100), (1, 200, 3000), (2, 1700, 448)]
 
 
 @pytest.mark.parametrize("kind", ["noise", "few"])
