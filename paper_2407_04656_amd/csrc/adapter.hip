@@ -52,7 +52,7 @@ inline int factor_units(const lz_adapter_shape* s) { return s->T / factor_chunk(
 
 // fp32 sizes that are no whole 16-byte pieces are copied to the next ones that are, with zeros around them, where the products are large
 // enough to pay for it: by single elements the products run at 25 to 30 TFLOP/s.  11575 x 1967 x 1325, rank 14: 1228 us by elements,
-// PADUS so; 1021 x 500 x 1301 67 and 61.
+// 667 so; 1021 x 500 x 1301 67 and 61.
 inline int up4(int v) { return (v + 3) / 4 * 4; }
 inline bool padded(const lz_adapter_shape* s) {
   return s->dtype == LZ_F32 && (s->d_in % 4 != 0 || s->d_out % 4 != 0 || s->rank % 4 != 0) && s->T >= 256 &&
@@ -523,7 +523,7 @@ int32_t sort_with_tables(const AdapterWorkspace& w, const lz_adapter_shape* s, h
 // ---- bf16 kernels
 
 // A token's adapter is read by its own waves where that is up to 64 MB in all: the tile kernel takes the adapters of 64 tokens one after
-// the other.  252 tokens of as many requests, 105 adapters of rank 8, 2048 x 3392: a training step 368 us by tiles, 129 so.
+// the other.  252 tokens of as many requests, 105 adapters of rank 8, 2048 x 3392: a training step 368 us by tiles, 122 so.
 inline bool by_token(const lz_adapter_shape* s, int d) { return (long long)s->T * s->rank * d <= (32ll << 20) && s->T <= 65535; }
 
 int32_t low_rank_mfma(const AdapterWorkspace& w, const lz_adapter_shape* s, const void* x, int d, const void* a, const float* scale, void* h,

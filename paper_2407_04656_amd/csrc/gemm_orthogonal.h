@@ -334,7 +334,7 @@ __global__ __launch_bounds__(kOrthoThreads) void join_gram_kernel(OrthoArgs a) {
 }
 
 // GRAM of few matrices has few tiles and a long sum: so many workgroups share a tile that the chip's places are taken, with 16 steps
-// each at least (a step of one 448 x 7488 matrix in two planes, 28 tiles of 351 steps, 547 us without, SPLITUS so).
+// each at least (a step of one 448 x 7488 matrix in two planes, 28 tiles of 351 steps, 547 us without, 301 so).
 template <int KIND, int PLANES>
 int32_t launch_ortho_narrow(OrthoArgs a, long long tiles, hipStream_t st) {
   if (tiles > 0x7FFFFFF0ll) return LZ_ESHAPE;

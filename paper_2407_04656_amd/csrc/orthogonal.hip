@@ -20,13 +20,10 @@ inline bool shape_ok(const lz_orthogonal_shape* s) {
 
 inline int small_side(const lz_orthogonal_shape* s) { return s->rows < s->cols ? s->rows : s->cols; }
 
-// A step in one launch pays where launches are what bounds it.  Sides of 65 to 128 hold a CU's LDS alone there: past 1024 blocks of
-// columns bf16 matrices run as wider ones do (48 of 75 x 3587, a step of fp32 weights: 852 us thin, THINUS so); fp32 ones stay, whose
-// long sums are the more exact there.
-inline bool use_thin(const lz_orthogonal_shape* s) {
-  const int small = small_side(s), large = s->rows < s->cols ? s->cols : s->rows;
-  return small <= kThinMost && (small <= 64 || s->dtype == LZ_F32 || (long long)s->n * (up64(large) / kThinBlock) <= 1024);
-}
+// A step in one launch pays where launches are what bounds it.  Sides of 65 to 128 hold a CU's LDS alone there: bf16 matrices run as wider
+// ones do (43 of 128 x 1408 386 us thin, 174 so; a step of 48 of 75 x 3587 852 and 557; four of 128 x 1024 138 and 94), fp32 ones
+// stay, whose long sums are the more exact there (8 of 128 x 256 92 us as wider ones, 78 so).
+inline bool use_thin(const lz_orthogonal_shape* s) { return small_side(s) <= (s->dtype == LZ_F32 ? kThinMost : 64); }
 
 struct OrthoWorkspace {
   double* sums;     // [n, norm_blocks()]
@@ -320,9 +317,10 @@ int32_t run(const Source& source, const float* old, const lz_orthogonal_shape* s
     const int32_t rc = lz::launch_status();
     if (rc != LZ_OK) return rc;
     const int sp = thin_side(small_side(shape));
-    return sp == 32   ? run_thin<Elem, UPDATE, PLANES, 32>(source, z, steps, n_steps, eps, out, update, w, st)
-           : sp == 64 ? run_thin<Elem, UPDATE, PLANES, 64>(source, z, steps, n_steps, eps, out, update, w, st)
-                      : run_thin<Elem, UPDATE, PLANES, 128>(source, z, steps, n_steps, eps, out, update, w, st);
+    if constexpr (sizeof(Elem) == 4)
+      if (sp == 128) return run_thin<Elem, UPDATE, PLANES, 128>(source, z, steps, n_steps, eps, out, update, w, st);
+    return sp == 32 ? run_thin<Elem, UPDATE, PLANES, 32>(source, z, steps, n_steps, eps, out, update, w, st)
+                    : run_thin<Elem, UPDATE, PLANES, 64>(source, z, steps, n_steps, eps, out, update, w, st);
   }
   if (whole && !z.tall && z.cols % 8 == 0) {
     const unsigned blocks = (unsigned)((size_t)z.sp * z.lp / 8 / 256 + 1);

@@ -1,4 +1,4 @@
-// Orthogonalised updates of matrices whose shorter side is at most 128: a step in one launch.  Device code of orthogonal.hip, not
+// Orthogonalised updates of matrices whose shorter side is at most 64, fp32 ones 128: a step in one launch.  Device code of orthogonal.hip, not
 // part of the C ABI.
 //
 // G is small here, and every workgroup holds all of H = G - mu I in LDS.  It takes 64 columns of X at a time,
