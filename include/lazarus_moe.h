@@ -345,8 +345,8 @@ const char* lz_layer_refused(void);
  *
  * W dev [d_in, d_out] (input-major, as the experts' weights), a dev [n, rank, d_in], b dev [n, rank, d_out], scale dev [n] f32,
  * x dev [T, d_in], y dev [T, d_out].  dtype: of x, y, h, w, a, b and their gradients; products are summed in fp32, h is rounded
- * once to dtype, y once.  LZ_BF16 with d_in, d_out and rank multiples of 8 and 16-byte aligned tensors runs on bf16 matrix
- * instructions; everything else on fp32 ones.
+ * once to dtype, y once.  LZ_BF16 with d_in, d_out and rank multiples of 8, 16-byte aligned tensors and T * max(d_in, d_out), d_in * d_out
+ * and n * rank * max(d_in, d_out) below 2^30 runs on bf16 matrix instructions; everything else on fp32 ones.
  *   T >= 0, d_in, d_out >= 1, 1 <= rank <= 1024, 1 <= n <= 4096, T * max(d_in, d_out) < 2^40, LZ_ESHAPE otherwise. */
 typedef struct {
   int32_t T, d_in, d_out, rank, n, dtype;
@@ -393,7 +393,7 @@ typedef struct {
 size_t lz_orthogonal_workspace_bytes(const lz_orthogonal_shape* shape);
 
 /* out[i] = the matrix g[i] after `steps` steps.  coef host [steps, 3], 1 <= steps <= 16; LZ_EINVAL for coefficients that can
- * take a singular value of [0, 1], or an intermediate product, past 2.8.
+ * take a singular value of [0, 1], or an intermediate product, past 3.9.
  *   g, out dev [n, rows, cols] of shape->dtype; they may be the same memory.  A matrix of zeros stays zero (eps > 0).
  * Products take their factors in 16-bit floating point, of 11 bits where the result is rounded to bf16 and, for LZ_F32, in two
  * parts of 11 bits each; sums are fp32. */

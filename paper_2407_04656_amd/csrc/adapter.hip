@@ -27,7 +27,8 @@ inline int chunks_of(int T) { return (T + chunk_tokens(T) - 1) / chunk_tokens(T)
 inline bool whole_pieces(const lz_adapter_shape* s) {
   const long long d = s->d_in > s->d_out ? s->d_in : s->d_out, most = (1ll << 30) - 4096;  // elements
   return s->dtype == LZ_BF16 && s->d_in % 8 == 0 && s->d_out % 8 == 0 && s->rank % 8 == 0 && s->T * d < most &&
-         (long long)s->d_in * s->d_out < most && (long long)s->n * s->rank * d < most && (long long)s->T * s->rank < most;
+         (long long)s->d_in * s->d_out < most && (long long)s->n * s->rank * d < most && (long long)s->T * s->rank < most &&
+         (long long)(ceil_div(s->d_in, kFactorCols) + ceil_div(s->d_out, kFactorCols)) * ceil_div(s->rank, 64) <= 65535;  // a grid's second side
 }
 // (the wide kernel's first two K steps are the base's)
 inline bool narrow_tiles(const lz_adapter_shape* s, int n_out, int K) { return use_narrow(s->T, 1, n_out) || K <= BK; }
@@ -43,12 +44,14 @@ inline int low_rank_splits(const lz_adapter_shape* s, int d) {
   const long long fill = 512 / (tiles > 0 ? tiles : 1);
   return (int)(fill < 1 ? 1 : fill < most ? fill : most);
 }
-// Rows of a unit of the factors' gradients.
-inline int factor_chunk(int T) {
-  const int even = (T / 16 + 63) / 64 * 64;
+// Rows of a unit of the factors' gradients: as many as leave the chip its 512 workgroups, which every column tile of either gradient
+// multiplies (units of an adapter add up through memory).
+inline int factor_chunk(const lz_adapter_shape* s) {
+  const int tiles = (ceil_div(s->d_in, kFactorCols) + ceil_div(s->d_out, kFactorCols)) * ceil_div(s->rank, 64);
+  const int units = tiles < 512 ? 512 / tiles : 1, even = (s->T / units + 63) / 64 * 64;
   return even < 256 ? 256 : even < kMostChunk ? even : kMostChunk;
 }
-inline int factor_units(const lz_adapter_shape* s) { return s->T / factor_chunk(s->T) + s->n; }
+inline int factor_units(const lz_adapter_shape* s) { return s->T / factor_chunk(s) + s->n; }
 
 // fp32 sizes that are no whole 16-byte pieces are copied to the next ones that are, with zeros around them, where the products are large
 // enough to pay for it: by single elements the products run at 25 to 30 TFLOP/s.  11575 x 1967 x 1325, rank 14: 1228 us by elements,
@@ -164,8 +167,8 @@ __global__ __launch_bounds__(256) void copy_jobs_kernel(CopyJobs jobs) {
   const long long all = (long long)j.count * j.to_rows;
   for (long long r = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); r < all; r += (long long)gridDim.x * 4) {
     const int m = (int)(r / j.to_rows), row = (int)(r - (long long)m * j.to_rows);
-    const float* const from = j.from + ((size_t)m * j.rows + row) * j.cols;
-#pragma unroll 4
+    const float* const from = j.from + ((size_t)m * j.rows + (row < j.rows ? row : 0)) * j.cols;
+#pragma unroll 16
     for (int c = threadIdx.x & 63; c < j.to_cols; c += 64) j.to[(size_t)r * j.to_cols + c] = row < j.rows && c < j.cols ? from[c] : 0.f;
   }
 }
@@ -208,11 +211,15 @@ __global__ __launch_bounds__(1024) void scan_ids_kernel(int32_t* __restrict__ co
   for (int a0 = 0; a0 <= n; a0 += 1024) {
     const int a = a0 + tid;
     int total = 0;
-    for (int c = 0; a <= n && c < chunks; ++c) {
-      int32_t& at = counts[(size_t)c * (n + 1) + a];
-      const int here = at;
-      at = total;
-      total += here;
+    for (int c0 = 0; a <= n && c0 < chunks; c0 += 16) {  // 16 chunks' counts on their way at a time
+      int here[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) here[i] = c0 + i < chunks ? counts[(size_t)(c0 + i) * (n + 1) + a] : 0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        if (c0 + i < chunks) counts[(size_t)(c0 + i) * (n + 1) + a] = total;
+        total += here[i];
+      }
     }
     const int incl = lz::wave_scan(total, [](int x, int y) { return x + y; });
     // an adapter without tokens has a unit of no rows: its gradients are zeros
@@ -494,7 +501,7 @@ int32_t sort_tokens(const AdapterWorkspace& w, const lz_adapter_shape* s, hipStr
   const size_t lds = 4 * (size_t)(n + 1);
   hipLaunchKernelGGL(count_ids_kernel, dim3(chunks), dim3(64), lds, st, ids ? ids : w.ids, T, n, chunk, w.ids, w.counts, status);
   hipLaunchKernelGGL(scan_ids_kernel, dim3(1), dim3(1024), 0, st, w.counts, chunks, n, T, w.first, w.all, w.unit_first, w.unit_adapter,
-                     factor_chunk(T));
+                     factor_chunk(s));
   hipLaunchKernelGGL(place_ids_kernel, dim3(chunks), dim3(64), lds, st, w.ids, T, n, chunk, w.counts, w.first, w.order, w.row_of);
   return lz::launch_status();
 }
@@ -586,7 +593,7 @@ int32_t backward_mfma(const AdapterWorkspace& w, const lz_adapter_shape* s, cons
   f.f[0] = FactorArgs{(const uint16_t*)w.dh, (const uint16_t*)x, (uint16_t*)da, w.factor_part[0], s->d_in, ceil_div(s->d_in, kFactorCols)};
   f.f[1] = FactorArgs{(const uint16_t*)h, (const uint16_t*)dy, (uint16_t*)db, w.factor_part[1], s->d_out, ceil_div(s->d_out, kFactorCols)};
   f.first = w.first, f.order = w.order, f.unit_first = w.unit_first, f.unit_adapter = w.unit_adapter;
-  f.n = s->n, f.rank = s->rank, f.rank_tiles = ceil_div(s->rank, 64), f.chunk = factor_chunk(s->T);
+  f.n = s->n, f.rank = s->rank, f.rank_tiles = ceil_div(s->rank, 64), f.chunk = factor_chunk(s);
   rc = allow_lds<factor_gradient_kernel>(kFactorLds);
   if (rc != LZ_OK) return rc;
   hipLaunchKernelGGL(factor_gradient_kernel, dim3(factor_units(s), (f.f[0].n_tiles + f.f[1].n_tiles) * f.rank_tiles), dim3(256), kFactorLds, st, f);
