@@ -62,7 +62,7 @@ struct Update {
 enum { THIN_FIRST = 0, THIN_STEP = 1, THIN_LAST = 2 };
 constexpr int kThinMost = 128;     // shorter side
 constexpr int kThinBlock = 64;     // columns at a time
-constexpr int kThinMostParts = 16; // workgroups of a matrix
+constexpr int kThinParts = 16;     // workgroups of a matrix, up to 32 blocks of columns
 
 struct ThinArgs {
   const double* sums;     // FIRST: of squares, norm_blocks of a matrix
@@ -343,11 +343,16 @@ __global__ __launch_bounds__(kThinThreads<SP>) void thin_step_kernel(ThinArgs a,
 
 inline int thin_side(int small) { return small <= 32 ? 32 : small <= 64 ? 64 : 128; }
 // Workgroups of a matrix: those that fill the chip twice, a block of columns each at least, and not so many that adding up their parts
-// of G is what they do.
+// of G is what they do.  P of them take blocks / P times a block's time and P times a part's, one about eight of the other, which is
+// least at P = sqrt(8 blocks).  Five steps, 16, 32, 64 of them: 32 x 65536 in bf16 390, 215, 136 us; 128 x 16384 in fp32 532, 371, 371;
+// 32 x 8192 70, 52, 52; 64 x 4096 in fp32 94, 80, 89; a step of 100 x 3000 197, 217, 231; 16 of 64 x 2048 93, 127 (32 fill the
+// chip twice).
 inline int thin_parts(int n, int columns) {
   const int fill = (512 + n - 1) / n, blocks = columns / kThinBlock;
-  const int most = fill < blocks ? fill : blocks;
-  return most < kThinMostParts ? most : kThinMostParts;
+  int parts = kThinParts;
+  while (parts < fill && (long long)parts * parts < 8LL * blocks) ++parts;
+  parts = parts < fill ? parts : fill;
+  return parts < blocks ? parts : blocks;
 }
 
 template <typename Elem, bool UPDATE, int MODE, int SP, int PLANES>
