@@ -100,6 +100,17 @@ def test_many_tiles(size, dtype):
     test_orthogonalize(size, dtype, "noise")
 
 
+# thin ones of so many columns that their workgroups are more than sixteen
+LONG = [(1, 24, 9001), (1, 20001, 20), (3, 64, 5000), (1, 100, 6007), (40, 16, 3000)]
+
+
+@pytest.mark.parametrize("kind", ["noise", "few"])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("size", LONG, ids=lambda s: "x".join(map(str, s)))
+def test_long_thin_matrices(size, dtype, kind):
+    test_orthogonalize(size, dtype, kind)
+
+
 @pytest.mark.parametrize("coef", [CUBIC, ((2.0, -1.5, 0.5),) * 3, ((1.0, 0.0, 0.0),), ((0.0, 0.0, 1.0),), ((1.0, -2.0, 0.25),),
                                   ((3.4445, -4.7750, 2.0315),) * 3 + ((1.875, -1.25, 0.375),) * 2], ids=str)
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
